@@ -364,6 +364,93 @@ int halo_mha_forward_ahead(const halo_mha_shape *shape, const void *x, const voi
                            int32_t *n_surv_next, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * Serving a batch of sequences over a paged cache: appending tokens, attending over the pages, and the norms around a block.  With the
+ * caller's projections these make an attention block for T sequences, next to an FFN that takes T tokens; surviving heads are those of a mask
+ * from halo_build_group_mask with G = n_heads, as in the attention block above.
+ *
+ * The cache is two pools of pages, k_pages and v_pages, each [n_pages][n_kv_heads][page_size][head_dim] (dtype): one head's tokens of a page
+ * are consecutive rows.  page_table [n_seq][max_pages] int32 lists each sequence's pages in order: position p lies in page
+ * page_table[seq][p / page_size], row p % page_size.  Pages may be shared between sequences, in any order.  An entry outside [0, n_pages)
+ * is no page: nothing is written to it or read from it.  Entries past a sequence's length are not used, whatever they hold, and rows of the pools past it do
+ * not change a result, whatever they hold (NaN among it).
+ *
+ * halo_paged_shape: n_heads <= 256 query heads, n_kv_heads of the cache (n_heads a multiple: query head h uses head h / (n_heads / n_kv_heads)),
+ * head_dim a multiple of 16 up to 256, page_size a power of two from 16 to 4096, n_pages >= 1, max_pages >= 1 with max_pages * page_size <= 2^30,
+ * dtype HALO_F32 or HALO_BF16.
+ */
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim;
+    int32_t page_size, n_pages, max_pages;
+    int32_t dtype;
+} halo_paged_shape;
+
+/*
+ * Table of rotation angles' cosines and sines for halo_paged_append.  HOST pointers, no GPU work: computed in double, rounded once.
+ *   table [n_pos][2][rotary_dim / 2] float: cos and sin of  p * theta^(-2 i / rotary_dim),  i < rotary_dim / 2.
+ * The caller copies it to the device, or makes one of its own (scaled or interpolated frequencies).
+ * Errors: HALO_ERR_NULL, HALO_ERR_ARG (n_pos < 0, rotary_dim < 2 or odd, theta not positive and finite).
+ */
+int halo_rope_table(int32_t n_pos, int32_t rotary_dim, double theta, float *table);
+
+/*
+ * Appends N new tokens of any sequences to their caches, one launch.  Token i belongs to sequence seq[i] (seq NULL: to sequence i) and has position pos[i]:
+ *   q_out[i] = R(pos[i]) q[i],   K row of the token = R(pos[i]) k[i],   V row of the token = v[i]
+ * for every head, where R(p) turns the pairs (a, b) of a head's first rotary_dim elements by the angle of position p,
+ *   (a, b) -> (a cos - b sin, b cos + a sin),
+ * element i < rotary_dim / 2 with element i + rotary_dim / 2, or (rope_pairs != 0) element 2i with element 2i + 1; the elements
+ * from rotary_dim on stay.  Computed in float, rounded once.
+ *   q [N][n_heads][head_dim], k, v [N][n_kv_heads][head_dim]: one token's heads are dense, tokens are *_stride elements apart (views of a
+ *       fused projection's output: no copies); tokens are 16-byte aligned.
+ *   q_out [N][n_heads][head_dim] dense; must not overlap q.  q and q_out may both be NULL: the cache alone is written.
+ *   pos [N], seq [N] int32; page_table [n_seq][max_pages]
+ *   rope [rope_len][2][rotary_dim / 2] float (halo_rope_table), rotary_dim a multiple of 16 up to head_dim; NULL = no rotation
+ *       (rope_len and rotary_dim are then ignored).
+ * A token with a sequence outside [0, n_seq), a position outside [0, max_pages * page_size) or (with a table) [0, rope_len), or whose page is no page, is padding:
+ * it writes nothing to the cache and its q_out is 0.  Two tokens of one position of one page leave either's values.
+ * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N < 0, n_seq < 1, strides shorter than a token or misaligned, bad
+ * rotary_dim or rope_len < 1, q_out == q, misaligned pointers), HALO_ERR_HIP.
+ */
+int halo_paged_append(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                      const int32_t *page_table, const float *rope, int32_t rope_len, int32_t rotary_dim, int32_t rope_pairs,
+                      void *q_out, void *k_pages, void *v_pages, void *stream);
+
+/*
+ * Attention of one new token of each of T sequences over its pages (its own key and value already appended):
+ *   out[t][h] = sum_j p_j V_j,   p = softmax_j(scale * q[t][h] . K_j),   j over positions 0 .. lens[t]-1
+ * Scores, softmax and sums are float32; with bf16 the probabilities are rounded to bf16 for the product with the values.
+ *   q [T][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [T][n_heads][head_dim] dense
+ *   page_table [T][max_pages], lens [T] int32 on the device
+ *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
+ *   mask [T][n_heads] uint8: a head whose byte is 0 gives out = 0, and the cache of heads without a surviving query is not read; NULL = all survive.
+ * Positions in pages that are no pages count as absent.  A sequence without positions gives out = 0.
+ * How the work is cut depends on the arguments that the host sees (T, max_len, the shape) and, for long ones, on the lengths; results do not depend on timing.
+ * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (T outside 0..4096, max_len, stride, alignment, scale not finite, or more than
+ * 2^30 tiles of 16 positions in all), HALO_ERR_WORKSPACE, HALO_ERR_HIP.  halo_paged_workspace_bytes: the workspace of up to T sequences; 0 for
+ * invalid arguments.
+ */
+size_t halo_paged_workspace_bytes(const halo_paged_shape *shape, int32_t T);
+
+int halo_paged_attention(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const void *k_pages,
+                         const void *v_pages, const int32_t *page_table, const int32_t *lens, int32_t max_len, const uint8_t *mask,
+                         float scale, void *out, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * What stands between two blocks, one launch, one pass over the rows: the norm after a block with its gate, the scaled residual, the norm before the next block,
+ *   u = post_norm ? n(y[t]) * w_post : y[t],   n(z) = z / sqrt(mean(z^2) + eps)
+ *   h_out[t] = res_scale * h[t] + gate * u,    x[t] = n(h_out[t]) * w_pre
+ * in float; h_out and x are each rounded once (x from the unrounded sum).
+ *   h, h_out [T][d] h_dtype (the residual stream; h_out may be h), y, x [T][d] dtype; w_post, w_pre [d] dtype, NULL = 1;
+ *   gate dtype, NULL = 1: [d], or with gate_per_token != 0 [T][d].
+ * h, y and gate are read and h_out, x written once.  x may be y.  h_dtype is HALO_F32 or dtype.
+ * Errors: HALO_ERR_NULL, HALO_ERR_DTYPE, HALO_ERR_ARG (T < 0, d not a multiple of 8 in 8..32768, eps negative or NaN, res_scale not finite,
+ * misaligned pointers), HALO_ERR_HIP.
+ */
+int halo_block_norm(const void *h, const void *y, const void *w_post, const void *gate, const void *w_pre, void *h_out, void *x,
+                    int32_t T, int32_t d, int32_t dtype, int32_t h_dtype, int32_t post_norm, int32_t gate_per_token, float res_scale,
+                    float eps, void *stream);
+
+/*
  * Benchmark aid (not part of the paper's method).  Between halo_profile_begin and
  * halo_profile_end every call of halo_group_sparse_ffn / halo_ffn_forward brackets the
  * FFN's dominant kernel -- the gate/up projection, which streams two thirds of the

@@ -549,3 +549,115 @@ int halo_ref_ffn_forward(const float *x, int32_t T, int32_t d, int32_t G, int32_
     if (rc) return rc;
     return halo_ref_group_sparse_ffn(x, T, d, G, gs, Wg, Wu, WdT, mask, y);
 }
+
+/* ------------------------------------------------------------------------- */
+/* A batch of sequences over a paged cache.                                    */
+/*                                                                           */
+/* Pools of pages [n_pages][n_kv][page][D]; table [n_seq][max_pages] lists the */
+/* pages of each sequence.  An entry outside [0, n_pages) is no page.          */
+/* ------------------------------------------------------------------------- */
+static int64_t paged_at(const int32_t *table_row, int32_t max_pages, int32_t n_pages, int32_t n_kv, int32_t page, int32_t D,
+                        int32_t head, int64_t pos)
+{
+    if (pos < 0 || pos / page >= max_pages) return -1;
+    const int32_t id = table_row[pos / page];
+    if (id < 0 || id >= n_pages) return -1;
+    return ((((int64_t)id * n_kv + head) * page) + pos % page) * D;
+}
+
+/* One head turned by the angles whose cosines and sines are cs[0..half-1], cs[half..2*half-1]. */
+static void turn(const float *x, const float *cs, int32_t half, int32_t pairs, int32_t D, double *out)
+{
+    for (int32_t i = 0; i < D; ++i) out[i] = (double)x[i];
+    for (int32_t i = 0; i < half; ++i) {
+        const int32_t a = pairs ? 2 * i : i, b = pairs ? 2 * i + 1 : i + half;
+        const double c = (double)cs[i], s = (double)cs[half + i];
+        out[a] = (double)x[a] * c - (double)x[b] * s;
+        out[b] = (double)x[b] * c + (double)x[a] * s;
+    }
+}
+
+/* q [N][Hq][D], k, v [N][n_kv][D] dense; rope [rope_len][2][half] or NULL; everything in double, nothing rounded. */
+int halo_ref_paged_append(int32_t N, int32_t Hq, int32_t n_kv, int32_t D, int32_t page, int32_t n_pages, int32_t max_pages,
+                          const float *q, const float *k, const float *v, const int32_t *pos, const int32_t *seq,
+                          int32_t n_seq, const int32_t *table, const float *rope, int32_t rope_len, int32_t half,
+                          int32_t pairs, double *q_out, double *k_pages, double *v_pages)
+{
+    for (int32_t i = 0; i < N; ++i) {
+        const int32_t s = seq ? seq[i] : i;
+        const int in_reach = s >= 0 && s < n_seq && pos[i] >= 0 && (!rope || pos[i] < rope_len);
+        const int64_t there = in_reach ? paged_at(table + (int64_t)s * max_pages, max_pages, n_pages, n_kv, page, D, 0, pos[i]) : -1;
+        const float *cs = rope && there >= 0 ? rope + (int64_t)pos[i] * 2 * half : NULL;
+        const int32_t turned = cs ? half : 0;
+        for (int32_t h = 0; h < Hq; ++h) {
+            double *to = q_out + ((int64_t)i * Hq + h) * D;
+            turn(q + ((int64_t)i * Hq + h) * D, cs, turned, pairs, D, to);
+            if (there < 0) memset(to, 0, sizeof(double) * (size_t)D);
+        }
+        for (int32_t h = 0; h < n_kv && there >= 0; ++h) {
+            const int64_t at = paged_at(table + (int64_t)s * max_pages, max_pages, n_pages, n_kv, page, D, h, pos[i]);
+            turn(k + ((int64_t)i * n_kv + h) * D, cs, turned, pairs, D, k_pages + at);
+            for (int32_t e = 0; e < D; ++e) v_pages[at + e] = (double)v[((int64_t)i * n_kv + h) * D + e];
+        }
+    }
+    return REF_OK;
+}
+
+/* One new token of each of T sequences: o_h = sum_j p_j V_j over the positions 0 .. len-1 that have a page. */
+int halo_ref_paged_attention(int32_t T, int32_t Hq, int32_t n_kv, int32_t D, int32_t page, int32_t n_pages, int32_t max_pages,
+                             const float *q, const float *k_pages, const float *v_pages, const int32_t *table,
+                             const int32_t *lens, const uint8_t *mask, double scale, double *out)
+{
+    const int32_t group = Hq / n_kv;
+#pragma omp parallel for collapse(2) schedule(dynamic)
+    for (int32_t t = 0; t < T; ++t)
+        for (int32_t h = 0; h < Hq; ++h) {
+            double *o = out + ((int64_t)t * Hq + h) * D;
+            memset(o, 0, sizeof(double) * (size_t)D);
+            if ((mask && !mask[(int64_t)t * Hq + h]) || lens[t] <= 0) continue;
+            const float *qh = q + ((int64_t)t * Hq + h) * D;
+            const int32_t *row = table + (int64_t)t * max_pages;
+            double *s = (double *)malloc(sizeof(double) * (size_t)lens[t]), top = -INFINITY, sum = 0.0;
+            for (int32_t j = 0; j < lens[t]; ++j) {
+                const int64_t at = paged_at(row, max_pages, n_pages, n_kv, page, D, h / group, j);
+                double d = 0.0;
+                for (int32_t e = 0; at >= 0 && e < D; ++e) d += (double)qh[e] * (double)k_pages[at + e];
+                s[j] = at < 0 ? -INFINITY : d * scale;
+                if (s[j] > top) top = s[j];
+            }
+            for (int32_t j = 0; j < lens[t]; ++j) {
+                const int64_t at = paged_at(row, max_pages, n_pages, n_kv, page, D, h / group, j);
+                if (at < 0) continue;
+                const double p = exp(s[j] - top);
+                sum += p;
+                for (int32_t e = 0; e < D; ++e) o[e] += p * (double)v_pages[at + e];
+            }
+            for (int32_t e = 0; e < D && sum != 0.0; ++e) o[e] /= sum;
+            free(s);
+        }
+    return REF_OK;
+}
+
+/* u = post ? n(y) w_post : y;  h' = res_scale h + gate u;  x = n(h') w_pre;  n(z) = z / sqrt(mean z^2 + eps). */
+int halo_ref_block_norm(int32_t T, int32_t d, const float *h, const float *y, const float *w_post, const float *gate,
+                        int32_t gate_per_token, const float *w_pre, int32_t post, double res_scale, double eps, double *h_out,
+                        double *x)
+{
+    for (int64_t t = 0; t < T; ++t) {
+        double sq = 0.0;
+        for (int32_t e = 0; e < d; ++e) sq += (double)y[t * d + e] * (double)y[t * d + e];
+        const double ry = post ? 1.0 / sqrt(sq / d + eps) : 1.0;
+        sq = 0.0;
+        for (int32_t e = 0; e < d; ++e) {
+            double u = (double)y[t * d + e] * ry;
+            if (post && w_post) u *= (double)w_post[e];
+            if (gate) u *= (double)gate[gate_per_token ? t * d + e : e];
+            const double z = res_scale * (double)h[t * d + e] + u;
+            h_out[t * d + e] = z;
+            sq += z * z;
+        }
+        const double rz = 1.0 / sqrt(sq / d + eps);
+        for (int32_t e = 0; e < d; ++e) x[t * d + e] = h_out[t * d + e] * rz * (w_pre ? (double)w_pre[e] : 1.0);
+    }
+    return REF_OK;
+}

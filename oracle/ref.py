@@ -234,3 +234,51 @@ def mha_decode(x, Wq, Wk, Wv, WoT, k_cache, v_cache, pos: int, mask=None, cache_
     if rc != 0:
         raise ValueError("halo_ref_mha_decode rejected its arguments")
     return y
+
+
+def paged_append(q, k, v, pos, seq, table, rope, pairs, k_pages, v_pages):
+    """Widened inputs; rope [rope_len][2][half] or None; seq or None.  Returns q_out and the pools afterwards, in double."""
+    q, k, v = _f32(q), _f32(k), _f32(v)
+    table, pos = (np.ascontiguousarray(a, dtype=np.int32) for a in (table, pos))
+    seq = None if seq is None else np.ascontiguousarray(seq, dtype=np.int32)
+    rope = None if rope is None else _f32(rope)
+    kp, vp = (np.array(p, dtype=np.float64, order="C") for p in (k_pages, v_pages))
+    out = np.full(q.shape, np.nan)
+    n_pages, n_kv, page, D = kp.shape
+    i = C.c_int32
+    rc = lib().halo_ref_paged_append(
+        i(q.shape[0]), i(q.shape[1]), i(n_kv), i(D), i(page), i(n_pages), i(table.shape[1]), _p(q, C.c_float), _p(k, C.c_float),
+        _p(v, C.c_float), _p(pos, C.c_int32), _p(seq, C.c_int32), i(table.shape[0]), _p(table, C.c_int32), _p(rope, C.c_float),
+        i(0 if rope is None else rope.shape[0]), i(0 if rope is None else rope.shape[2]), i(int(pairs)), _p(out, C.c_double),
+        _p(kp, C.c_double), _p(vp, C.c_double))
+    assert rc == 0
+    return out, kp, vp
+
+
+def paged_attention(q, k_pages, v_pages, table, lens, mask=None, scale=None) -> np.ndarray:
+    q, kp, vp = _f32(q), _f32(k_pages), _f32(v_pages)
+    table, lens = (np.ascontiguousarray(a, dtype=np.int32) for a in (table, lens))
+    mask = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint8)
+    T, Hq, D = q.shape
+    n_pages, n_kv, page, _ = kp.shape
+    out = np.full(q.shape, np.nan)
+    i = C.c_int32
+    rc = lib().halo_ref_paged_attention(
+        i(T), i(Hq), i(n_kv), i(D), i(page), i(n_pages), i(table.shape[1]), _p(q, C.c_float), _p(kp, C.c_float),
+        _p(vp, C.c_float), _p(table, C.c_int32), _p(lens, C.c_int32), _p(mask, C.c_uint8),
+        C.c_double(D ** -0.5 if scale is None else scale), _p(out, C.c_double))
+    assert rc == 0
+    return out
+
+
+def block_norm(h, y, w_post=None, gate=None, w_pre=None, post=False, res_scale=1.0, eps=1e-5):
+    h, y = _f32(h), _f32(y)
+    w_post, gate, w_pre = (None if a is None else _f32(a) for a in (w_post, gate, w_pre))
+    T, d = h.shape
+    h_out, x = np.full(h.shape, np.nan), np.full(h.shape, np.nan)
+    i = C.c_int32
+    rc = lib().halo_ref_block_norm(i(T), i(d), _p(h, C.c_float), _p(y, C.c_float), _p(w_post, C.c_float), _p(gate, C.c_float),
+                                   i(int(gate is not None and gate.ndim == 2)), _p(w_pre, C.c_float), i(int(post)),
+                                   C.c_double(res_scale), C.c_double(eps), _p(h_out, C.c_double), _p(x, C.c_double))
+    assert rc == 0
+    return h_out, x

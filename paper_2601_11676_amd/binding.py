@@ -43,6 +43,31 @@ class MhaShape:
         self.c = _CMhaShape(d, n_heads, head_dim, rank, code)
 
 
+class _CPagedShape(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32)]
+
+
+class PagedShape:
+    """halo_paged_shape: n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype ('f32' | 'bf16')."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_pages: int,
+                 dtype: str = "bf16"):
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
+        self.page_size, self.n_pages, self.max_pages, self.dtype = page_size, n_pages, max_pages, dtype
+        code = {"f32": HALO_F32, "bf16": HALO_BF16}.get(dtype, -1)
+        self.c = _CPagedShape(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, code)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    @property
+    def pool(self):
+        """Shape of k_pages and of v_pages."""
+        return (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+
+
 class Shape:
     """halo_shape: d, ffn, group_size, n_groups, rank, dtype ('f32' | 'bf16')."""
 
@@ -125,6 +150,18 @@ def load_library():
     lib.halo_mha_forward_ahead.restype = C.c_int
     lib.halo_mha_forward_ahead.argtypes = [pm, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp,
                                            i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    pp = C.POINTER(_CPagedShape)
+    i64, f32 = C.c_int64, C.c_float
+    lib.halo_rope_table.restype = C.c_int
+    lib.halo_rope_table.argtypes = [i32, i32, C.c_double, vp]
+    lib.halo_paged_append.restype = C.c_int
+    lib.halo_paged_append.argtypes = [pp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.halo_paged_workspace_bytes.restype = sz
+    lib.halo_paged_workspace_bytes.argtypes = [pp, i32]
+    lib.halo_paged_attention.restype = C.c_int
+    lib.halo_paged_attention.argtypes = [pp, i32, vp, i64, vp, vp, vp, vp, i32, vp, f32, vp, vp, sz, vp]
+    lib.halo_block_norm.restype = C.c_int
+    lib.halo_block_norm.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, f32, vp]
     lib.halo_profile_begin.restype = C.c_int
     lib.halo_profile_begin.argtypes = [i32, i32]
     lib.halo_profile_end.restype = C.c_int
@@ -363,6 +400,89 @@ def halo_mha_forward_ahead(shape: MhaShape, x, Wq, Wk, Wv, Wo, k_cache, v_cache,
         _ptr(group_dev_next), _ptr(mask_next), _ptr(surv_idx_next), _ptr(n_surv_next), _ptr(workspace),
         workspace.numel(), _stream(stream))
     _check("halo_mha_forward_ahead", rc)
+
+
+def halo_rope_table(n_pos: int, rotary_dim: int, theta: float = 10000.0) -> np.ndarray:
+    """Host-only: cosines and sines of the positions' angles, float32 [n_pos][2][rotary_dim / 2]."""
+    out = np.empty((max(int(n_pos), 0), 2, max(int(rotary_dim) // 2, 0)), dtype=np.float32)
+    _check("halo_rope_table", load_library().halo_rope_table(int(n_pos), int(rotary_dim), float(theta),
+                                                             out.ctypes.data_as(C.c_void_p)))
+    return out
+
+
+def _heads(t: torch.Tensor, heads: int, dim: int, dtype):
+    """Address and token stride of [tokens][heads][dim], whose tokens may lie apart (a view of a fused projection's rows)."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+        raise ValueError(f"[tokens][{heads}][{dim}] of {dtype} expected")
+    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
+        raise ValueError("a token's heads must be dense")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def _typed(t: Optional[torch.Tensor], dtype, *shape):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+        raise ValueError(f"{list(shape)} of {dtype} expected")
+    return _ptr(t)
+
+
+def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
+                      rope_pairs: bool = False, seq=None, stream=None) -> None:
+    """q [N][n_heads][head_dim] (or None, with q_out), k, v [N][n_kv_heads][head_dim]; rope as halo_rope_table gives it, on the
+    device; seq None: token i belongs to sequence i."""
+    N, dt = k.shape[0], shape.torch_dtype
+    pk, sk = _heads(k, shape.n_kv_heads, shape.head_dim, dt)
+    pv, sv = _heads(v, shape.n_kv_heads, shape.head_dim, dt)
+    pq, sq = (None, 0) if q is None else _heads(q, shape.n_heads, shape.head_dim, dt)
+    if v.shape[0] != N or (q is not None and q.shape[0] != N):
+        raise ValueError("q, k and v must hold the same tokens")
+    n_seq = page_table.shape[0]
+    if seq is None and n_seq < N:
+        raise ValueError("without seq, every token needs a row of the page table")
+    rows, half = (0, 0) if rope is None else (rope.shape[0], rope.shape[2])
+    rc = load_library().halo_paged_append(
+        shape.c, N, pq, sq, pk, sk, pv, sv, _typed(pos, torch.int32, N), _typed(seq, torch.int32, N), n_seq,
+        _typed(page_table, torch.int32, n_seq, shape.max_pages), _typed(rope, torch.float32, rows, 2, half), rows, 2 * half,
+        int(rope_pairs), _typed(q_out, dt, N, shape.n_heads, shape.head_dim), _typed(k_pages, dt, *shape.pool),
+        _typed(v_pages, dt, *shape.pool), _stream(stream))
+    _check("halo_paged_append", rc)
+
+
+def halo_paged_workspace_bytes(shape: PagedShape, T: int) -> int:
+    return int(load_library().halo_paged_workspace_bytes(shape.c, int(T)))
+
+
+def halo_paged_attention(shape: PagedShape, q, k_pages, v_pages, page_table, lens, max_len: int, out, workspace, mask=None,
+                         scale: Optional[float] = None, stream=None) -> None:
+    """scale None: 1 / sqrt(head_dim)."""
+    T, dt = q.shape[0], shape.torch_dtype
+    pq, sq = _heads(q, shape.n_heads, shape.head_dim, dt)
+    if scale is None:
+        scale = shape.head_dim ** -0.5
+    rc = load_library().halo_paged_attention(
+        shape.c, T, pq, sq, _typed(k_pages, dt, *shape.pool), _typed(v_pages, dt, *shape.pool),
+        _typed(page_table, torch.int32, T, shape.max_pages), _typed(lens, torch.int32, T), int(max_len),
+        _typed(mask, torch.uint8, T, shape.n_heads), float(scale), _typed(out, dt, T, shape.n_heads, shape.head_dim),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    _check("halo_paged_attention", rc)
+
+
+def halo_block_norm(h, y, x, h_out=None, post_norm: bool = False, w_post=None, gate=None, res_scale: float = 1.0, w_pre=None,
+                    eps: float = 1e-5, stream=None) -> None:
+    """h [T][d] (h_out None: in place), y, x [T][d]; gate [d] or [T][d]."""
+    T, d = h.shape
+    codes = {torch.float32: HALO_F32, torch.bfloat16: HALO_BF16}
+    dt = y.dtype
+    if gate is not None and gate.dim() not in (1, 2):
+        raise ValueError("gate must be [d] or [T][d]")
+    per_token = gate is not None and gate.dim() == 2
+    h_out = h if h_out is None else h_out
+    rc = load_library().halo_block_norm(
+        _ptr(h), _typed(y, dt, T, d), _typed(w_post, dt, d), _typed(gate, dt, *((T, d) if per_token else (d,))),
+        _typed(w_pre, dt, d), _typed(h_out, h.dtype, T, d), _typed(x, dt, T, d), T, d, codes.get(dt, -1), codes.get(h.dtype, -1),
+        int(post_norm), int(per_token), float(res_scale), float(eps), _stream(stream))
+    _check("halo_block_norm", rc)
 
 
 class _Recorder:
