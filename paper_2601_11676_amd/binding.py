@@ -15,6 +15,7 @@ _lib = None
 _tls = threading.local()      # prepared(): the recorder standing in for the library in this thread, if any
 
 HALO_F32, HALO_BF16 = 0, 1
+_CODES = {torch.float32: HALO_F32, torch.bfloat16: HALO_BF16}
 
 
 class HaloError(RuntimeError):
@@ -57,15 +58,8 @@ class PagedShape:
         self.page_size, self.n_pages, self.max_pages, self.dtype = page_size, n_pages, max_pages, dtype
         code = {"f32": HALO_F32, "bf16": HALO_BF16}.get(dtype, -1)
         self.c = _CPagedShape(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, code)
-
-    @property
-    def torch_dtype(self):
-        return torch.float32 if self.dtype == "f32" else torch.bfloat16
-
-    @property
-    def pool(self):
-        """Shape of k_pages and of v_pages."""
-        return (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+        self.pool = (n_pages, n_kv_heads, page_size, head_dim)       # shape of k_pages and of v_pages
 
 
 class Shape:
@@ -411,42 +405,55 @@ def halo_rope_table(n_pos: int, rotary_dim: int, theta: float = 10000.0) -> np.n
 
 
 def _heads(t: torch.Tensor, heads: int, dim: int, dtype):
-    """Address and token stride of [tokens][heads][dim], whose tokens may lie apart (a view of a fused projection's rows)."""
+    """Address, token stride and tokens of [tokens][heads][dim], whose tokens may lie apart (a view of a fused projection's rows)."""
     if not t.is_cuda:
         raise ValueError("device tensor expected")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+    size = t.shape
+    if len(size) != 3 or size[1] != heads or size[2] != dim or t.dtype is not dtype:
         raise ValueError(f"[tokens][{heads}][{dim}] of {dtype} expected")
-    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
+    apart, head, one = t.stride()
+    if one != 1 or (head != dim and heads > 1):                      # head_dim is 16 at least
         raise ValueError("a token's heads must be dense")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+    return t.data_ptr(), apart if size[0] > 1 else heads * dim, size[0]
 
 
-def _typed(t: Optional[torch.Tensor], dtype, *shape):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+def _typed(t: torch.Tensor, dtype, shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{list(shape)} of {dtype} expected")
-    return _ptr(t)
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    if not t.is_contiguous():
+        raise ValueError("contiguous tensor expected")
+    return t.data_ptr()
 
 
 def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
                       rope_pairs: bool = False, seq=None, stream=None) -> None:
     """q [N][n_heads][head_dim] (or None, with q_out), k, v [N][n_kv_heads][head_dim]; rope as halo_rope_table gives it, on the
     device; seq None: token i belongs to sequence i."""
-    N, dt = k.shape[0], shape.torch_dtype
-    pk, sk = _heads(k, shape.n_kv_heads, shape.head_dim, dt)
-    pv, sv = _heads(v, shape.n_kv_heads, shape.head_dim, dt)
-    pq, sq = (None, 0) if q is None else _heads(q, shape.n_heads, shape.head_dim, dt)
-    if v.shape[0] != N or (q is not None and q.shape[0] != N):
+    dt, dim, n_kv = shape.torch_dtype, shape.head_dim, shape.n_kv_heads
+    pk, sk, N = _heads(k, n_kv, dim, dt)
+    pv, sv, Nv = _heads(v, n_kv, dim, dt)
+    pq, sq, Nq, po = None, 0, N, None
+    if q is not None:
+        pq, sq, Nq = _heads(q, shape.n_heads, dim, dt)
+    if Nv != N or Nq != N:
         raise ValueError("q, k and v must hold the same tokens")
+    if q_out is not None:
+        po = _typed(q_out, dt, (N, shape.n_heads, dim))
     n_seq = page_table.shape[0]
     if seq is None and n_seq < N:
         raise ValueError("without seq, every token needs a row of the page table")
-    rows, half = (0, 0) if rope is None else (rope.shape[0], rope.shape[2])
+    pr, rows, half = None, 0, 0
+    if rope is not None:
+        rows, _, half = rope.shape
+        pr = _typed(rope, torch.float32, (rows, 2, half))
     rc = load_library().halo_paged_append(
-        shape.c, N, pq, sq, pk, sk, pv, sv, _typed(pos, torch.int32, N), _typed(seq, torch.int32, N), n_seq,
-        _typed(page_table, torch.int32, n_seq, shape.max_pages), _typed(rope, torch.float32, rows, 2, half), rows, 2 * half,
-        int(rope_pairs), _typed(q_out, dt, N, shape.n_heads, shape.head_dim), _typed(k_pages, dt, *shape.pool),
-        _typed(v_pages, dt, *shape.pool), _stream(stream))
-    _check("halo_paged_append", rc)
+        shape.c, N, pq, sq, pk, sk, pv, sv, _typed(pos, torch.int32, (N,)), None if seq is None else _typed(seq, torch.int32, (N,)),
+        n_seq, _typed(page_table, torch.int32, (n_seq, shape.max_pages)), pr, rows, 2 * half, 1 if rope_pairs else 0, po,
+        _typed(k_pages, dt, shape.pool), _typed(v_pages, dt, shape.pool), _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_append", rc)
 
 
 def halo_paged_workspace_bytes(shape: PagedShape, T: int) -> int:
@@ -456,33 +463,35 @@ def halo_paged_workspace_bytes(shape: PagedShape, T: int) -> int:
 def halo_paged_attention(shape: PagedShape, q, k_pages, v_pages, page_table, lens, max_len: int, out, workspace, mask=None,
                          scale: Optional[float] = None, stream=None) -> None:
     """scale None: 1 / sqrt(head_dim)."""
-    T, dt = q.shape[0], shape.torch_dtype
-    pq, sq = _heads(q, shape.n_heads, shape.head_dim, dt)
+    dt, pool = shape.torch_dtype, shape.pool
+    pq, sq, T = _heads(q, shape.n_heads, shape.head_dim, dt)
     if scale is None:
         scale = shape.head_dim ** -0.5
     rc = load_library().halo_paged_attention(
-        shape.c, T, pq, sq, _typed(k_pages, dt, *shape.pool), _typed(v_pages, dt, *shape.pool),
-        _typed(page_table, torch.int32, T, shape.max_pages), _typed(lens, torch.int32, T), int(max_len),
-        _typed(mask, torch.uint8, T, shape.n_heads), float(scale), _typed(out, dt, T, shape.n_heads, shape.head_dim),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
-    _check("halo_paged_attention", rc)
+        shape.c, T, pq, sq, _typed(k_pages, dt, pool), _typed(v_pages, dt, pool),
+        _typed(page_table, torch.int32, (T, shape.max_pages)), _typed(lens, torch.int32, (T,)), max_len,
+        None if mask is None else _typed(mask, torch.uint8, (T, shape.n_heads)), scale,
+        _typed(out, dt, (T, shape.n_heads, shape.head_dim)), _ptr(workspace), workspace.nbytes, _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_attention", rc)
 
 
 def halo_block_norm(h, y, x, h_out=None, post_norm: bool = False, w_post=None, gate=None, res_scale: float = 1.0, w_pre=None,
                     eps: float = 1e-5, stream=None) -> None:
     """h [T][d] (h_out None: in place), y, x [T][d]; gate [d] or [T][d]."""
-    T, d = h.shape
-    codes = {torch.float32: HALO_F32, torch.bfloat16: HALO_BF16}
-    dt = y.dtype
-    if gate is not None and gate.dim() not in (1, 2):
-        raise ValueError("gate must be [d] or [T][d]")
-    per_token = gate is not None and gate.dim() == 2
-    h_out = h if h_out is None else h_out
+    size, dt, ht = h.shape, y.dtype, h.dtype
+    T, d = size
+    pg, per_token = None, 0
+    if gate is not None:
+        per_token = 1 if gate.dim() == 2 else 0
+        pg = _typed(gate, dt, size if per_token else (d,))
+    ph = _ptr(h)
     rc = load_library().halo_block_norm(
-        _ptr(h), _typed(y, dt, T, d), _typed(w_post, dt, d), _typed(gate, dt, *((T, d) if per_token else (d,))),
-        _typed(w_pre, dt, d), _typed(h_out, h.dtype, T, d), _typed(x, dt, T, d), T, d, codes.get(dt, -1), codes.get(h.dtype, -1),
-        int(post_norm), int(per_token), float(res_scale), float(eps), _stream(stream))
-    _check("halo_block_norm", rc)
+        ph, _typed(y, dt, size), None if w_post is None else _typed(w_post, dt, (d,)), pg,
+        None if w_pre is None else _typed(w_pre, dt, (d,)), ph if h_out is None else _typed(h_out, ht, size), _typed(x, dt, size),
+        T, d, _CODES.get(dt, -1), _CODES.get(ht, -1), 1 if post_norm else 0, per_token, res_scale, eps, _stream(stream))
+    if rc:
+        raise HaloError("halo_block_norm", rc)
 
 
 class _Recorder:

@@ -4,9 +4,10 @@
 // 4 * group / 2 operations a byte in bf16, where this card has about 200 to spare.
 //
 // A wave is the worker.  The queries of one cache head (up to 16: a unit) are the 16 columns of the matrix instruction, so that grouped heads share
-// what is read; with one query a column of 16 is used, and the matrix cores still outrun the stream.  Nothing passes through LDS on the way:
-//   S^T = K Q^T      rows = tokens, columns = queries.  A lane (row = lane & 15) holds 16-byte pieces of its token's row as they lie in memory.
-//                    The result leaves lane (c = lane & 15, g = lane >> 4) with query c's scores of the tokens 4g .. 4g+3 of each 16.
+// what is read; with one query a column of 16 is used, and the matrix cores still outrun the stream.
+//   S^T = K Q^T      rows = tokens, columns = queries.  A lane (c = lane & 15, g = lane >> 4) wants pieces (16 bytes) of token c's row; loaded
+//                    like that, an instruction touches 16 rows.  So whole rows are loaded, and pass through a part of LDS that is the wave's own.
+//                    The result leaves the lane with query c's scores of the tokens 4g .. 4g+3 of each 16.
 //   O^T += V^T P^T   the sum over tokens may take them in any order, so the operand P^T is what the lane already holds: its own
 //                    scores' exponentials.  V^T then wants, in lane (c, g), those tokens' values of one dimension.  The lane loads
 //                    whole 16-byte pieces of the same tokens' rows (piece c: coalesced) and pairs up halves of registers; the dimension
@@ -28,9 +29,8 @@ namespace halo {
 namespace {
 
 constexpr int kCols = 16;                            // queries of a unit at most: columns of the matrix instruction
-constexpr int kStreamWaves = 4;                      // waves of a workgroup of the even shares
-constexpr int kStreamGrid = 512;                     // two such workgroups on each of 256 compute units
-constexpr int kMaxWorkers = kStreamGrid * kStreamWaves;
+constexpr int kStreamGrid = 512;                     // workgroups of the even shares: two on each of 256 compute units
+constexpr int kMaxWorkers = kStreamGrid * kTeam;
 constexpr int kMaxSeqs = 4096;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -43,7 +43,7 @@ struct AttendArgs {
     const uint8_t *mask;
     void *out;
     float *part, *stats;                             // partial results of cut pairs: [slot][rows][D], [slot][rows][max, sum]
-    int32_t *plan;                                   // [0] tiles per worker, [1 + t] first tile of sequence t
+    int32_t *plan;                                   // [0] tiles per worker, [1] all tiles, [2 + t] first tile of sequence t
     int64_t q_stride;
     PagePool pool;
     int T, n_heads, group, n_qt, n_units, rows, D, max_pages, max_len;
@@ -61,90 +61,135 @@ __device__ __forceinline__ float xor_max16_32(float v)
     return fmaxf(as_f(b[0]), as_f(b[1]));
 }
 
-// The running softmax of one unit over bf16 rows: 32 tokens a step.  DP = head dimension, or the next of 64, 128, 256 above it (EXACT false).
-template <int DP, bool EXACT>
+// 16 rows of one page: what a descriptor lets a lane read.  Rows that do not count lie past its end and read as zeros, whatever memory holds there
+// (a probability of 0 does not keep NaN out of a sum), and a page that does not exist is a descriptor of no bytes: loads need no condition.
+template <typename V, int POLICY>
+__device__ __forceinline__ V row_load(__amdgpu_buffer_rsrc_t rows, uint32_t at)
+{
+    if constexpr (sizeof(V) == 16)
+        return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, POLICY));
+    else
+        return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, POLICY));
+}
+
+// Which of the cache's rows carry the non-temporal hint: none, the values, both.  What passes through once should not push out what stays; with
+// caches that fit the dies' L2 the hint costs.  us, by the bytes of the call, none / values / both: 18 MB 9.4 / 11.3 / 11.6; 98 MB 19.4 / 18.5 / 19.3;
+// 134 MB 36.4 / 31.3 / 32.3; 738 MB 140 / 127 / 123; 1.7 GB 316 / 286 / 281.
+enum { kKeepAll = 0, kPassValues = 1, kPassBoth = 2 };
+
+// Keys on their way from whole rows, as they are loaded, to the lanes that multiply them: 16 rows of DP elements in LDS, piece p of row r at place
+// p ^ r (within 16), so that neither side meets a bank twice.  kRows rows a load; the same number of loads as of pieces a lane gets.
+template <typename Elem, int DP>
+struct KeyPlace {
+    static constexpr int kBytes = DP * sizeof(Elem), kPieces = kBytes / 16, kRows = 64 / kPieces, kLoads = kPieces / 4;
+    static constexpr int kTurn = (kPieces < 16 ? kPieces : 16) - 1;
+    uint32_t from, in, out;                          // offset in memory, places in LDS of the first load and of the first piece
+
+    __device__ __forceinline__ void place(int D, int lane)
+    {
+        const int row = lane / kPieces, piece = lane % kPieces, c = lane & 15, g = lane >> 4;
+        from = piece * 16 < D * (int)sizeof(Elem) ? (uint32_t)(row * D * (int)sizeof(Elem) + piece * 16) : kOutOfRange;
+        in = row * kBytes + ((piece ^ row) << 4);
+        out = c * kBytes + ((g ^ (c & kTurn)) << 4);
+    }
+    __device__ __forceinline__ uint32_t put(int i) const { return (in ^ ((i * kRows & kTurn) << 4)) + i * kRows * kBytes; }
+    __device__ __forceinline__ uint32_t get(int s) const { return out ^ (s << 6); }
+};
+
+// A step's keys: loaded rows in, the lane's pieces out.  A wave's LDS accesses keep their order: nothing to wait for in between.
+template <typename Core>
+__device__ __forceinline__ void turn_keys(Core &core)
+{
+#pragma unroll
+    for (int i = 0; i < Core::kSub; ++i)
+#pragma unroll
+        for (int s = 0; s < Core::KS; ++s) *reinterpret_cast<u32x4 *>(core.lds + i * 16 * core.keys.kBytes + core.keys.put(s)) = __builtin_bit_cast(u32x4, core.kf[i][s]);
+#pragma unroll
+    for (int i = 0; i < Core::kSub; ++i)
+#pragma unroll
+        for (int s = 0; s < Core::KS; ++s) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(core.lds + i * 16 * core.keys.kBytes + core.keys.get(s));
+            core.kf[i][s] = __builtin_bit_cast(std::remove_reference_t<decltype(core.kf[i][s])>, v);
+        }
+}
+
+// The running softmax of one unit over bf16 rows, kSub times 16 tokens a step.  DP = head dimension, or the next of 64, 128, 256 above it (EXACT false).
+template <int DP, bool EXACT, int HINT>
 struct CoreBf16 {
     typedef bf16_t Elem;
-    static constexpr int kTile = 32, kSub = 2;       // tokens a step, 16-token rows of the matrix instruction in it
+    static constexpr int kSub = DP > 64 ? 2 : 4, kTile = kSub * 16;      // rows of 128 and 64: 16 KiB of keys and values a step
     static constexpr int kItemWaves = DP > 128 ? 4 : 8;     // waves of a workgroup that takes a pair: rows of 256 need more than 256 registers
+    static constexpr int kWaves = DP > 128 ? 1 : 2;         // on a SIMD, for the same reason
+    static constexpr int kStage = kTile * DP * 2, kMostRows = kCols * DP * 4;    // LDS of a wave: a step's keys, in the end its part of the results
     static constexpr int KS = DP / 32;               // pieces of a key row in a lane
-    static constexpr int VEC = DP >= 128 ? 8 : 4, VH = DP >= 128 ? DP / 128 : 1, kAcc = VEC * VH;
+    static constexpr int VEC = DP > 64 ? 8 : 4, VH = DP > 128 ? 2 : 1, kAcc = VEC * VH;
     typedef std::conditional_t<VEC == 8, u32x4, u32x2> VPiece;
 
-    u32x4 qf[KS], kf[2][KS];
-    VPiece vf[8][VH];
+    u32x4 qf[KS], kf[kSub][KS];
+    VPiece vf[4 * kSub][VH];
     f32x4 acc[kAcc], sum;
     float m;
-    uint32_t koff[KS], voff[VH];
-    bool kin[KS];
+    KeyPlace<bf16_t, DP> keys;
+    char *lds;                                       // kStage bytes, the wave's own
+    uint32_t voff[VH];
     int D, c, g;
 
-    __device__ __forceinline__ void place(int d, int lane)
+    __device__ __forceinline__ void place(int d, int lane, char *own)
     {
         D = EXACT ? DP : d;
         c = lane & 15;
         g = lane >> 4;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int dim = s * 32 + g * 8;
-            kin[s] = EXACT || dim < D;
-            koff[s] = (uint32_t)(c * D + (kin[s] ? dim : 0)) * 2;
-        }
+        lds = own;
+        keys.place(D, lane);
 #pragma unroll
         for (int h = 0; h < VH; ++h) {
             const int dim = h * 16 * VEC + c * VEC;
-            voff[h] = (uint32_t)(g * 4 * D + (EXACT || dim < D ? dim : 0)) * 2;     // past the row's end: not stored
+            voff[h] = EXACT || dim < D ? (uint32_t)(g * 4 * D + dim) * 2 : kOutOfRange;
         }
     }
     __device__ __forceinline__ void begin(const bf16_t *q, int nq)
     {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            qf[s] = c < nq && kin[s] ? *reinterpret_cast<const u32x4 *>(q + c * D + s * 32 + g * 8) : u32x4{0u, 0u, 0u, 0u};
+        for (int s = 0; s < KS; ++s) {
+            const int dim = s * 32 + g * 8;
+            qf[s] = c < nq && (EXACT || dim < D) ? *reinterpret_cast<const u32x4 *>(q + c * D + dim) : u32x4{0u, 0u, 0u, 0u};
+        }
 #pragma unroll
         for (int j = 0; j < kAcc; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         sum = f32x4{0.f, 0.f, 0.f, 0.f};
         m = -INFINITY;
     }
-    __device__ __forceinline__ void load_k(const char *const (&base)[kSub])
+    __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kSub; ++i)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[i][s] = *reinterpret_cast<const u32x4 *>(base[i] + koff[s]);
+            for (int s = 0; s < KS; ++s) kf[i][s] = row_load<u32x4, HINT == kPassBoth ? kNt : 0>(rows[i], keys.from + s * keys.kRows * D * 2);
     }
-    __device__ __forceinline__ void load_v(const char *const (&base)[kSub])
+    __device__ __forceinline__ void load_v(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
-            for (int h = 0; h < VH; ++h)
-                vf[i][h] = *reinterpret_cast<const VPiece *>(base[i >> 2] + (i & 3) * D * 2 + voff[h]);
+            for (int h = 0; h < VH; ++h) vf[i][h] = row_load<VPiece, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 2);
     }
     static __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &acc)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
     }
-    __device__ __forceinline__ void scores(float (&x)[8])
+    // the lane's scores: 4i + r is token 16i + 4g + r of the step
+    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
     {
-        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        turn_keys(*this);
+        f32x4 s[kSub];
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                u32x4 a = kf[i][k];
-                if constexpr (!EXACT) a = kin[k] ? a : u32x4{0u, 0u, 0u, 0u};
-                s[i] = mfma(a, qf[k], s[i]);
-            }
+            for (int i = 0; i < kSub; ++i) s[i] = mfma(kf[i][k], qf[k], s[i]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3];
-    }
-    // token of the lane's e-th score, from the step's first
-    __device__ __forceinline__ int token(int e) const { return (e >> 2) * 16 + g * 4 + (e & 3); }
-    __device__ __forceinline__ void clear_v(int e)
-    {
-#pragma unroll
-        for (int h = 0; h < VH; ++h) vf[e][h] = VPiece{};
+        for (int e = 0; e < 4 * kSub; ++e) x[e] = s[e >> 2][e & 3];
     }
     __device__ __forceinline__ void rescale(float by)
     {
@@ -154,97 +199,98 @@ struct CoreBf16 {
     }
     // The probabilities are rounded to bf16 here, and the sum is of the rounded ones: weights that add up to one, so that a row with one
     // dominant token comes out as that token's values.
-    __device__ __forceinline__ void accumulate(const float (&p)[8])
+    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        auto pair = [&](float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); };
-        const u32x4 pf = {pair(p[0], p[1]), pair(p[2], p[3]), pair(p[4], p[5]), pair(p[6], p[7])};
+        auto pair = [](float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); };
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-        sum = mfma(ones, pf, sum);
 #pragma unroll
-        for (int h = 0; h < VH; ++h)
+        for (int o = 0; o < 4 * kSub; o += 8) {
+            const u32x4 pf = {pair(p[o], p[o + 1]), pair(p[o + 2], p[o + 3]), pair(p[o + 4], p[o + 5]), pair(p[o + 6], p[o + 7])};
+            sum = mfma(ones, pf, sum);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-                u32x4 a;
+            for (int h = 0; h < VH; ++h)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) a[t] = __builtin_amdgcn_perm(vf[2 * t + 1][h][j >> 1], vf[2 * t][h][j >> 1], sel);
-                acc[h * VEC + j] = mfma(a, pf, acc[h * VEC + j]);
-            }
+                for (int j = 0; j < VEC; ++j) {
+                    const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+                    u32x4 a;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        a[t] = __builtin_amdgcn_perm(vf[o + 2 * t + 1][h][j >> 1], vf[o + 2 * t][h][j >> 1], sel);
+                    acc[h * VEC + j] = mfma(a, pf, acc[h * VEC + j]);
+                }
+        }
     }
     __device__ __forceinline__ float total() const { return sum[0]; }
 };
 
-// The same over float rows: 16 tokens a step, every operand one float a lane.
-template <int DP, bool EXACT>
+// The same over float rows: every operand of the matrix instruction is one float a lane.
+template <int DP, bool EXACT, int HINT>
 struct CoreF32 {
     typedef float Elem;
-    static constexpr int kTile = 16, kSub = 1;
-    static constexpr int kItemWaves = DP > 128 ? 4 : 8;
+    static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
+    static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
     static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
 
-    f32x4 qf[KS], kf[KS], vf[4][VH], acc[kAcc];
+    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[kAcc];
     float m, l;
-    uint32_t koff[KS], voff[VH];
-    bool kin[KS];
+    KeyPlace<float, DP> keys;
+    char *lds;
+    uint32_t voff[VH];
     int D, c, g;
 
-    __device__ __forceinline__ void place(int d, int lane)
+    __device__ __forceinline__ void place(int d, int lane, char *own)
     {
         D = EXACT ? DP : d;
         c = lane & 15;
         g = lane >> 4;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            kin[s] = EXACT || s * 16 < D;            // D is a multiple of 16
-            koff[s] = (uint32_t)(c * D + (kin[s] ? s * 16 + g * 4 : 0)) * 4;
-        }
+        lds = own;
+        keys.place(D, lane);
 #pragma unroll
         for (int h = 0; h < VH; ++h) {
             const int dim = h * 64 + c * 4;
-            voff[h] = (uint32_t)(g * 4 * D + (EXACT || dim < D ? dim : 0)) * 4;
+            voff[h] = EXACT || dim < D ? (uint32_t)(g * 4 * D + dim) * 4 : kOutOfRange;
         }
     }
     __device__ __forceinline__ void begin(const float *q, int nq)
     {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            qf[s] = c < nq && kin[s] ? *reinterpret_cast<const f32x4 *>(q + c * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+            qf[s] = c < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + c * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kAcc; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.0f;
         m = -INFINITY;
     }
-    __device__ __forceinline__ void load_k(const char *const (&base)[kSub])
+    __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const f32x4 *>(base[0] + koff[s]);
+        for (int i = 0; i < kSub; ++i)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[i][s] = row_load<f32x4, HINT == kPassBoth ? kNt : 0>(rows[i], keys.from + s * keys.kRows * D * 4);
     }
-    __device__ __forceinline__ void load_v(const char *const (&base)[kSub])
+    __device__ __forceinline__ void load_v(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
-            for (int h = 0; h < VH; ++h) vf[i][h] = *reinterpret_cast<const f32x4 *>(base[0] + i * D * 4 + voff[h]);
+            for (int h = 0; h < VH; ++h) vf[i][h] = row_load<f32x4, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 4);
     }
-    __device__ __forceinline__ void scores(float (&x)[4])
+    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
     {
-        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        turn_keys(*this);
+        f32x4 s[kSub][2];
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) s[i][0] = s[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = EXACT || kin[k] ? kf[k][e] : 0.0f;
-                s[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, qf[k][e], s[e & 1], 0, 0, 0);
-            }
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = s[0][e] + s[1][e];
-    }
-    __device__ __forceinline__ int token(int e) const { return g * 4 + e; }
-    __device__ __forceinline__ void clear_v(int e)
-    {
+                for (int i = 0; i < kSub; ++i)
+                    s[i][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][k][e], qf[k][e], s[i][e & 1], 0, 0, 0);
 #pragma unroll
-        for (int h = 0; h < VH; ++h) vf[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4 * kSub; ++e) x[e] = s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3];
     }
     __device__ __forceinline__ void rescale(float by)
     {
@@ -252,11 +298,12 @@ struct CoreF32 {
         for (int j = 0; j < kAcc; ++j) acc[j] *= by;
         l *= by;
     }
-    __device__ __forceinline__ void accumulate(const float (&p)[4])
+    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
     {
-        l += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4 * kSub; i += 4) l += (p[i] + p[i + 1]) + (p[i + 2] + p[i + 3]);
+#pragma unroll
+        for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
             for (int j = 0; j < kAcc; ++j)
                 acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[i], acc[j], 0, 0, 0);
@@ -264,49 +311,50 @@ struct CoreF32 {
     __device__ __forceinline__ float total() const { return xor_add<16>(xor_add<32>(l)); }
 };
 
-// The pages of one sequence: 64 entries of its row of the table at a time, one a lane.  All calls are wave-uniform.
-struct PageRow {
+// The tiles first, first + stride, .. (count of them) of one sequence that a wave takes, and the pages of their 16-token parts: 64 parts at a time, one
+// a lane.  All calls are wave-uniform.
+template <typename Core>
+struct Tiles {
+    static constexpr int kHeld = kWave / Core::kSub;
     const int32_t *row;
-    int n, first, id, lane;
+    int max_pages, shift, first, stride, from, id, lane;
 
-    __device__ __forceinline__ PageRow(const AttendArgs &a, int t, int page, int lane)
-        : row(a.table + (int64_t)t * a.max_pages), n(a.max_pages), lane(lane)
+    __device__ __forceinline__ Tiles(const AttendArgs &a, int t, int first, int stride, int lane)
+        : row(a.table + (int64_t)t * a.max_pages), max_pages(a.max_pages), shift(a.pool.page_shift), first(first), stride(stride), lane(lane)
     {
-        fetch(page);
+        fetch(0);
     }
-    __device__ __forceinline__ void fetch(int page)
+    __device__ __forceinline__ int position(int i) const { return (first + i * stride) * Core::kTile; }
+    __device__ __forceinline__ void fetch(int i)
     {
-        first = page;
-        id = page + lane < n ? row[page + lane] : -1;
+        from = i;
+        const int page = (position(i + lane / Core::kSub) + lane % Core::kSub * 16) >> shift;
+        id = page < max_pages ? row[page] : -1;
         asm volatile("" : "+v"(id));                 // waited for here, and not at every use of a step that fetched nothing
     }
-    __device__ __forceinline__ int operator[](int page)
-    {
-        if (page - first >= kWave) fetch(page);
-        return __builtin_amdgcn_readlane(id, page - first);
-    }
+    __device__ __forceinline__ int page(int i, int part) const { return __builtin_amdgcn_readlane(id, (i - from) * Core::kSub + part); }
 };
 
-// Where a step's rows are, and whether all of them count.  Rows of a page that does not exist are replaced by the pool's first ones: loads need no
-// condition, and what they bring is masked.
 template <typename Core>
 struct Step {
-    const char *k[Core::kSub], *v[Core::kSub];
+    __amdgpu_buffer_rsrc_t k[Core::kSub], v[Core::kSub];
     int live[Core::kSub];                            // tokens of the 16 that count
     bool whole;
 
-    __device__ __forceinline__ Step(const AttendArgs &a, PageRow &pages, int kv, int len, int tile)
+    __device__ __forceinline__ Step(const AttendArgs &a, Tiles<Core> &tiles, int kv, int len, int i)
     {
+        constexpr int kBytes = sizeof(typename Core::Elem);
+        if (i - tiles.from >= Tiles<Core>::kHeld) tiles.fetch(i);
         whole = true;
 #pragma unroll
-        for (int i = 0; i < Core::kSub; ++i) {
-            const int pos = tile * Core::kTile + i * 16;
-            const int64_t row = pos < len ? paged_row(a.pool, pages[pos >> a.pool.page_shift], kv, pos) : -1;
-            live[i] = row < 0 ? 0 : len - pos < 16 ? len - pos : 16;
-            whole = whole && live[i] == 16;
-            const int64_t at = (row < 0 ? 0 : row) * a.D * (int)sizeof(typename Core::Elem);
-            k[i] = static_cast<const char *>(a.k) + at;
-            v[i] = static_cast<const char *>(a.v) + at;
+        for (int p = 0; p < Core::kSub; ++p) {
+            const int pos = tiles.position(i) + p * 16;
+            const int64_t row = paged_row(a.pool, tiles.page(i, p), kv, pos);
+            live[p] = row < 0 ? 0 : max(0, min(len - pos, 16));
+            whole = whole && live[p] == 16;
+            const int64_t at = (row < 0 ? 0 : row) * a.D * kBytes;
+            k[p] = buffer_of(static_cast<const char *>(a.k) + at, live[p] * a.D * kBytes);
+            v[p] = buffer_of(static_cast<const char *>(a.v) + at, live[p] * a.D * kBytes);
         }
     }
 };
@@ -320,7 +368,7 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
     for (int e = 0; e < N; ++e) x[e] *= scale2;
     if (!st.whole) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = (core.token(e) & 15) < st.live[e >> 2] ? x[e] : -INFINITY;
+        for (int e = 0; e < N; ++e) x[e] = core.g * 4 + (e & 3) < st.live[e >> 2] ? x[e] : -INFINITY;
     }
     float top = x[0];
 #pragma unroll
@@ -337,37 +385,26 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
     for (int e = 0; e < N; ++e) x[e] = __builtin_amdgcn_exp2f(x[e] - m);
 }
 
-// Tiles [b, e) of sequence t, unit (kv, first query): the next step's keys are asked for as soon as this one's are used up, and its
+// `count` tiles of a sequence against the queries in `core`: the next step's keys are asked for as soon as this one's are used up, and its
 // values after this one's.
 template <typename Core>
-__device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, int t, int kv, int len, int b, int e, int lane)
+__device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, Tiles<Core> &tiles, int kv, int len, int count)
 {
-    constexpr int N = 4 * Core::kSub;
-    PageRow pages(a, t, (b * Core::kTile) >> a.pool.page_shift, lane);
-    Step<Core> now(a, pages, kv, len, b);
+    float x[4 * Core::kSub];
+    Step<Core> now(a, tiles, kv, len, 0);
     core.load_k(now.k);
     core.load_v(now.v);
-    auto drop_absent = [&] {                         // probability 0, but whatever the row holds: not even NaN may reach the sums
-        if (!now.whole) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((core.token(i) & 15) >= now.live[i >> 2]) core.clear_v(i);
-        }
-    };
-    float x[N];
-    for (int tile = b; tile + 1 < e; ++tile) {
-        const Step<Core> next(a, pages, kv, len, tile + 1);
+    for (int i = 1; i < count; ++i) {
+        const Step<Core> next(a, tiles, kv, len, i);
         core.scores(x);
         core.load_k(next.k);
         softmax_step(core, now, a.scale2, x);
-        drop_absent();
         core.accumulate(x);
         core.load_v(next.v);
         now = next;
     }
     core.scores(x);
     softmax_step(core, now, a.scale2, x);
-    drop_absent();
     core.accumulate(x);
 }
 
@@ -423,68 +460,71 @@ __device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, f
         }
 }
 
-template <typename Core>
-__device__ __forceinline__ void store_out_rows(const AttendArgs &a, const Core &core, int t, const Unit &unit)
-{
-    const float l = core.total();
-    const bool alive = core.c < unit.nq && head_alive(a, t, unit.head + core.c);
-    // a sum of 0 is a row without positions; NaN has to come through
-    store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq,
-               !alive || l == 0.0f ? 0.0f : 1.0f / l);
-}
-
 // ---------------------------------------------------------------------------
 // one workgroup a pair
 // ---------------------------------------------------------------------------
+// What the waves of a workgroup have of one pair, joined from LDS: element i of the pair's rows (query i / D) and its query's maximum and sum.
+struct Joined {
+    float m, l, o;
+    __device__ __forceinline__ Joined(const float *part, int part_stride, const float2 *stats, int waves, int n, int i) : m(-INFINITY), l(0.0f), o(0.0f)
+    {
+        for (int w = 0; w < waves; ++w) m = fmaxf(m, stats[w * kCols + n].x);
+        for (int w = 0; w < waves; ++w) {
+            const float2 ml = stats[w * kCols + n];
+            if (ml.y == 0.0f) continue;              // no positions: nothing was stored
+            const float by = __builtin_amdgcn_exp2f(ml.x - m);
+            l += ml.y * by;
+            o += part[w * part_stride + i] * by;
+        }
+    }
+};
+
+// The waves take every kItemWaves-th tile, so that where a wave begins, and with it the pages it asks for first, does not wait for the length.
 template <typename Core>
 __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs a)
 {
-    constexpr int kItemWaves = Core::kItemWaves;
-    extern __shared__ __align__(16) float s_part[];  // [waves][rows][D], then [waves][16][max, sum]
-    float *s_stats = s_part + kItemWaves * a.rows * a.D;
+    constexpr int kWaves = Core::kItemWaves;
+    __shared__ __align__(16) char s_own[kWaves * Core::kStage];
+    __shared__ float2 s_stats[kWaves * kCols];       // maximum and sum
+    static_assert(Core::kStage >= Core::kMostRows, "a wave's results fit its part");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = blockIdx.x / a.n_units, u = blockIdx.x - t * a.n_units;
     const Unit unit(a, u);
-    const int len = paged_length(a.lens[t], a.max_len);
-    const int tiles = unit_alive(a, t, u) ? (len + Core::kTile - 1) / Core::kTile : 0;
-    const int b = tiles * wave / kItemWaves, e = tiles * (wave + 1) / kItemWaves;
     Core core;
-    core.place(a.D, lane);
+    core.place(a.D, lane, s_own + wave * Core::kStage);
+    float *const s_part = reinterpret_cast<float *>(s_own);
+    constexpr int kPart = Core::kStage / 4;
+    const int kept = a.mask && core.c < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + core.c] : !a.mask;
+    const int len = paged_length(a.lens[t], a.max_len);
     core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
-    if (b < e) attend_tiles(a, core, t, unit.kv, len, b, e, lane);
+    Tiles<Core> tiles(a, t, wave, kWaves, lane);
+    const int all = __ballot(kept != 0) ? (len + Core::kTile - 1) / Core::kTile : 0;
+    const int count = (all - wave + kWaves - 1) / kWaves;        // all < wave: none
+    if (count > 0) attend_tiles(a, core, tiles, unit.kv, len, count);
     const float l = core.total();
-    if (core.g == 0) {
-        s_stats[(wave * kCols + core.c) * 2] = core.m;
-        s_stats[(wave * kCols + core.c) * 2 + 1] = l;
-    }
-    if (b < e) store_rows(core, s_part + wave * a.rows * core.D, unit.nq, 1.0f);
+    if (core.g == 0) s_stats[wave * kCols + core.c] = make_float2(core.m, l);
+    if (count > 0) store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
     __syncthreads();
     typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D;
-    for (int i = threadIdx.x; i < unit.nq * core.D; i += kItemWaves * 64) {
+    for (int i = threadIdx.x; i < unit.nq * core.D; i += kWaves * 64) {
         const int n = i / core.D;
-        float top = -INFINITY, sum = 0.0f, o = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kItemWaves; ++w) top = fmaxf(top, s_stats[(w * kCols + n) * 2]);
-        for (int w = 0; w < kItemWaves; ++w) {
-            const float ml = s_stats[(w * kCols + n) * 2], ll = s_stats[(w * kCols + n) * 2 + 1];
-            if (ll == 0.0f) continue;                // no positions: nothing was stored
-            const float by = __builtin_amdgcn_exp2f(ml - top);
-            sum += ll * by;
-            o += s_part[(w * a.rows) * core.D + i] * by;
-        }
-        store_out(out + i, sum == 0.0f || !head_alive(a, t, unit.head + n) ? 0.0f : o / sum);
+        const Joined j(s_part, kPart, s_stats, kWaves, n, i);
+        store_out(out + i, j.l == 0.0f || !head_alive(a, t, unit.head + n) ? 0.0f : j.o / j.l);
     }
 }
 
 // ---------------------------------------------------------------------------
 // even shares of all tiles
 // ---------------------------------------------------------------------------
-// s_base[t] = tiles of the sequences before t, s_base[T] = all.  Called by the whole workgroup.
+// s_base[t] = tiles of the sequences before t, s_base[T] = all; s_len[t] = length.  Called by the whole workgroup.
 template <int kTile>
-__device__ __forceinline__ void line_up(const AttendArgs &a, int *s_base, int *s_wave)
+__device__ __forceinline__ void line_up(const AttendArgs &a, int *s_base, int *s_len, int *s_wave)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = kStreamWaves * 64;
-    for (int t = tid; t < a.T; t += threads) s_base[t] = a.mask ? 0 : a.n_units;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = kTeam * 64;
+    for (int t = tid; t < a.T; t += threads) {
+        s_base[t] = a.mask ? 0 : a.n_units;
+        s_len[t] = paged_length(a.lens[t], a.max_len);
+    }
     __syncthreads();
     if (a.mask) {
         for (int i = tid; i < a.T * a.n_units; i += threads) {
@@ -496,7 +536,7 @@ __device__ __forceinline__ void line_up(const AttendArgs &a, int *s_base, int *s
     const int each = (a.T + threads - 1) / threads, from = min(tid * each, a.T), to = min(from + each, a.T);
     int mine = 0;
     for (int t = from; t < to; ++t) {
-        const int n = s_base[t] * ((paged_length(a.lens[t], a.max_len) + kTile - 1) / kTile);
+        const int n = s_base[t] * ((s_len[t] + kTile - 1) / kTile);
         s_base[t] = mine;
         mine += n;
     }
@@ -542,33 +582,40 @@ struct AliveUnits {
 };
 
 template <typename Core>
-__global__ __launch_bounds__(kStreamWaves * 64) void attend_stream(AttendArgs a)
+__global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(AttendArgs a)
 {
-    __shared__ int s_base[kMaxSeqs + 1], s_wave[kStreamWaves];
-    line_up<Core::kTile>(a, s_base, s_wave);
+    __shared__ __align__(16) char s_own[kTeam * Core::kStage];
+    extern __shared__ int s_line[];                  // bases [T + 1], lengths [T]
+    __shared__ float2 s_stats[kTeam * kCols];
+    __shared__ int s_wave[kTeam];
+    __shared__ int4 s_last[kTeam];                   // the pair that a wave's share ends in: first tile (-1: none), tiles, sequence, unit
+    float *const s_part = reinterpret_cast<float *>(s_own);
+    constexpr int kPart = Core::kStage / 4;
+    int *const s_base = s_line, *const s_len = s_line + a.T + 1;
+    line_up<Core::kTile>(a, s_base, s_len, s_wave);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto base = [&](int t) { return __builtin_amdgcn_readfirstlane(s_base[t]); };
-    const int total = base(a.T), per = tiles_per_worker(total, gridDim.x * kStreamWaves, a.least);
+    const int total = base(a.T), per = tiles_per_worker(total, gridDim.x * kTeam, a.least);
     if (blockIdx.x == 0) {                           // for the second launch
-        for (int t = threadIdx.x; t < a.T; t += kStreamWaves * 64) a.plan[1 + t] = s_base[t];
-        if (threadIdx.x == 0) a.plan[0] = per;
+        for (int t = threadIdx.x; t < a.T; t += kTeam * 64) a.plan[2 + t] = s_base[t];
+        if (threadIdx.x == 0) a.plan[0] = per, a.plan[1] = total;
     }
-    const int worker = blockIdx.x * kStreamWaves + wave;
-    if ((int64_t)worker * per >= total) return;
-    int at = worker * per;
-    const int end = min(at + per, total);
+    const int worker = blockIdx.x * kTeam + wave;
+    int at = (int)min((int64_t)worker * per, (int64_t)total);
+    const int end = (int)min((int64_t)at + per, (int64_t)total);
     int lo = 0, hi = a.T;                            // the sequence whose tiles hold `at`: base[lo] <= at < base[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (base(mid) <= at) lo = mid; else hi = mid;
     }
     Core core;
-    core.place(a.D, lane);
+    core.place(a.D, lane, s_own + wave * Core::kStage);
     AliveUnits units;
+    int4 last = make_int4(-1, 0, 0, 0);
     for (int t = lo; at < end; ++t) {
         const int from = base(t), size = base(t + 1) - from;
         if (size == 0) continue;
-        const int len = paged_length(__builtin_amdgcn_readfirstlane(a.lens[t]), a.max_len);
+        const int len = __builtin_amdgcn_readfirstlane(s_len[t]);
         const int tiles = (len + Core::kTile - 1) / Core::kTile;
         int n = (at - from) / tiles;
         units.find(a, t, n, lane);
@@ -576,91 +623,111 @@ __global__ __launch_bounds__(kStreamWaves * 64) void attend_stream(AttendArgs a)
             const Unit unit(a, units.unit());
             const int offset = from + n * tiles, b = at - offset, e = min(tiles, end - offset);
             core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
-            attend_tiles(a, core, t, unit.kv, len, b, e, lane);
+            Tiles<Core> mine(a, t, b, 1, lane);
+            attend_tiles(a, core, mine, unit.kv, len, e - b);
             at = offset + e;
-            if (b == 0 && e == tiles) {
-                store_out_rows(a, core, t, unit);
-                continue;
-            }
-            const int64_t slot = partial_slot(worker, per, offset);
             const float l = core.total();
-            if (core.g == 0 && core.c < unit.nq)
-                *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + core.c) * 2) = make_float2(core.m, l);
-            store_rows(core, a.part + slot * a.rows * core.D, unit.nq, 1.0f);
+            if (b == 0 && e == tiles) {
+                // a sum of 0 is a row without positions; NaN has to come through
+                const bool alive = core.c < unit.nq && head_alive(a, t, unit.head + core.c);
+                store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq,
+                           !alive || l == 0.0f ? 0.0f : 1.0f / l);
+            } else if (at < end) {                   // the share goes on: a partial result of its own
+                const int64_t slot = 2 * (int64_t)worker;
+                if (core.g == 0 && core.c < unit.nq)
+                    *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + core.c) * 2) = make_float2(core.m, l);
+                store_rows(core, a.part + slot * a.rows * core.D, unit.nq, 1.0f);
+            } else {
+                last = make_int4(offset, tiles, t, units.unit());
+                if (core.g == 0) s_stats[wave * kCols + core.c] = make_float2(core.m, l);
+                store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
+            }
+        }
+    }
+    if (lane == 0) s_last[wave] = last;
+    __syncthreads();
+    for (int w = 0, waves; w < kTeam; w += waves) {  // the same for every thread
+        const int4 pair = s_last[w];
+        for (waves = 1; w + waves < kTeam && s_last[w + waves].x == pair.x; ++waves) {}
+        if (pair.x < 0) continue;
+        const Cut cut(pair.x, pair.y, per, total);
+        const Unit unit(a, pair.w);
+        const int64_t slot = 2 * (int64_t)(blockIdx.x * kTeam + w) + 1;
+        typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)pair.z * a.n_heads + unit.head) * core.D;
+        for (int i = threadIdx.x; i < unit.nq * core.D; i += kTeam * 64) {
+            const int n = i / core.D;
+            const Joined j(s_part + w * kPart, kPart, s_stats + w * kCols, waves, n, i);
+            if (cut.in_team) {
+                store_out(out + i, j.l == 0.0f || !head_alive(a, pair.z, unit.head + n) ? 0.0f : j.o / j.l);
+            } else {
+                a.part[slot * a.rows * core.D + i] = j.o;
+                if (i == n * core.D) *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + n) * 2) = make_float2(j.m, j.l);
+            }
         }
     }
 }
 
-// Joins the pairs that more than one worker had, and gives 0 to those that nobody had.  A workgroup a pair: its threads stand for four
-// dimensions of one query each, several of them sharing the partial results where there are threads to spare.
-template <typename Core>
+// A partial result taken into the running ones (m, l, o).
+__device__ __forceinline__ void take_in(float &m, float &l, float4 &o, const float2 &ml, const float4 &p)
+{
+    const float to = fmaxf(m, ml.x), use = to == -INFINITY ? 0.0f : to;
+    const float keep = __builtin_amdgcn_exp2f(m - use), by = __builtin_amdgcn_exp2f(ml.x - use);
+    l = l * keep + ml.y * by;
+    o.x = o.x * keep + p.x * by;
+    o.y = o.y * keep + p.y * by;
+    o.z = o.z * keep + p.z * by;
+    o.w = o.w * keep + p.w * by;
+    m = to;
+}
+
+// Joins the pairs that the first launch left in parts, and gives 0 to those that nobody had.  Workgroups (x) stand for pairs, cut by y; a thread stands
+// for four dimensions of one query, kShares threads of a workgroup for the same, each with its share of the parts.
+template <typename Elem, int kTile, int kShares>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
 {
+    constexpr int kQuads = 256 / kShares;
     __shared__ float4 s_o[256];
     __shared__ float2 s_ml[256];
-    typedef typename Core::Elem Elem;
-    const int lane = threadIdx.x & 63, tid = threadIdx.x;
+    const int lane = threadIdx.x & 63, tid = threadIdx.x, share = tid / kQuads;
     const int t = blockIdx.x / a.n_units, u = blockIdx.x - t * a.n_units;
     const Unit unit(a, u);
-    const int per = a.plan[0], from = a.plan[1 + t];
-    const int tiles = (paged_length(a.lens[t], a.max_len) + Core::kTile - 1) / Core::kTile;
+    const int per = a.plan[0], total = a.plan[1], from = a.plan[2 + t];
+    const int tiles = (paged_length(a.lens[t], a.max_len) + kTile - 1) / kTile;
     int rank = u;
-    bool alive = true;
+    bool any = tiles > 0;
     if (a.mask) {
         rank = 0;
         for (int block = 0; block <= u; block += 64) {
             const uint64_t bits = __ballot(block + lane < a.n_units && unit_alive(a, t, block + lane));
             rank += __popcll(u - block < 64 ? bits & ((1ull << (u - block)) - 1) : bits);
-            if (u - block < 64) alive = (bits >> (u - block)) & 1;
+            if (u - block < 64) any = any && ((bits >> (u - block)) & 1);
         }
     }
-    const int offset = from + rank * tiles;
-    const bool any = alive && tiles > 0;
-    const int w0 = any ? first_worker(offset, per) : 0, w1 = any ? last_worker(offset, tiles, per) : -1;
-    if (any && w0 == w1) return;                     // written by that worker
+    const Cut cut(any ? from + rank * tiles : 0, any ? tiles : 1, per, total);
+    if (any && (cut.whole || cut.in_team)) return;   // written out by the first launch
+    const int parts = any ? cut.parts() : 0, quads = unit.nq * (a.D / 4);
     Elem *out = static_cast<Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * a.D;
-    const int quads = unit.nq * (a.D / 4);           // at least 4
-    const int parts = quads < 256 ? 256 / quads : 1, part = quads < 256 ? tid / quads : 0;
-    for (int block = 0; block < quads; block += 256) {
-        const int i = quads < 256 ? tid - part * quads : block + tid;
-        const int n = min(i / (a.D / 4), unit.nq - 1);
+    for (int block = blockIdx.y * kQuads; block < quads; block += gridDim.y * kQuads) {
+        const int i = block + tid % kQuads, n = min(i, quads - 1) / (a.D / 4);
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i < quads && part < parts) {
+        if (i < quads)
 #pragma unroll 4
-            for (int w = w0 + part; w <= w1; w += parts) {
-                const int64_t slot = partial_slot(w, per, offset);
-                const float2 ml = *reinterpret_cast<const float2 *>(a.stats + (slot * a.rows + n) * 2);
-                const float4 p = *reinterpret_cast<const float4 *>(a.part + slot * a.rows * a.D + i * 4);
-                const float to = fmaxf(m, ml.x), use = to == -INFINITY ? 0.0f : to;
-                const float keep = __builtin_amdgcn_exp2f(m - use), by = __builtin_amdgcn_exp2f(ml.x - use);
-                l = l * keep + ml.y * by;
-                o.x = o.x * keep + p.x * by;
-                o.y = o.y * keep + p.y * by;
-                o.z = o.z * keep + p.z * by;
-                o.w = o.w * keep + p.w * by;
-                m = to;
+            for (int k = share; k < parts; k += kShares) {
+                const int64_t slot = cut.slot(k);
+                take_in(m, l, o, *reinterpret_cast<const float2 *>(a.stats + (slot * a.rows + n) * 2),
+                        *reinterpret_cast<const float4 *>(a.part + slot * a.rows * a.D + i * 4));
             }
-        }
-        if (parts > 1) {                             // the same for every thread
+        if constexpr (kShares > 1) {
+            __syncthreads();
             s_o[tid] = o;
             s_ml[tid] = make_float2(m, l);
             __syncthreads();
-            if (part == 0)
-                for (int k = 1; k < parts; ++k) {
-                    const float2 ml = s_ml[k * quads + tid];
-                    const float4 p = s_o[k * quads + tid];
-                    const float to = fmaxf(m, ml.x), use = to == -INFINITY ? 0.0f : to;
-                    const float keep = __builtin_amdgcn_exp2f(m - use), by = __builtin_amdgcn_exp2f(ml.x - use);
-                    l = l * keep + ml.y * by;
-                    o.x = o.x * keep + p.x * by;
-                    o.y = o.y * keep + p.y * by;
-                    o.z = o.z * keep + p.z * by;
-                    o.w = o.w * keep + p.w * by;
-                    m = to;
-                }
+            if (share == 0)
+#pragma unroll
+                for (int k = 1; k < kShares; ++k) take_in(m, l, o, s_ml[k * kQuads + tid], s_o[k * kQuads + tid]);
         }
-        if (part == 0 && i < quads) {
+        if (share == 0 && i < quads) {
             const bool none = l == 0.0f || !head_alive(a, t, unit.head + n);
             const float v[4] = {none ? 0.0f : o.x / l, none ? 0.0f : o.y / l, none ? 0.0f : o.z / l, none ? 0.0f : o.w / l};
             store_piece(out + i * 4, v);
@@ -679,40 +746,56 @@ struct PagedWorkspace {
     {
         const size_t group = s.n_heads / s.n_kv_heads, rows = group < kCols ? group : kCols;
         const size_t slots = 2 * (size_t)kMaxWorkers;
-        stats = align256(((size_t)T + 1) * sizeof(int32_t));
+        stats = align256(((size_t)T + 2) * sizeof(int32_t));
         part = stats + align256(slots * rows * 2 * sizeof(float));
         bytes = part + align256(slots * rows * s.head_dim * sizeof(float));
     }
 };
 
 template <typename Core>
-int launch_core(const AttendArgs &a, bool one_launch, int bound, hipStream_t s)
+int launch_item(const AttendArgs &a, hipStream_t s)
 {
-    if (one_launch) {
-        constexpr int kItemWaves = Core::kItemWaves;
-        const size_t lds = (size_t)kItemWaves * ((size_t)a.rows * a.D + 2 * kCols) * sizeof(float);
-        if (lds > 65536 &&
-            hipFuncSetAttribute(reinterpret_cast<const void *>(attend_item<Core>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-            return HALO_ERR_HIP;
-        attend_item<Core><<<dim3(a.T * a.n_units), dim3(kItemWaves * 64), lds, s>>>(a);
-    } else {
-        const int wanted = (bound + kStreamWaves * a.least - 1) / (kStreamWaves * a.least);
-        attend_stream<Core><<<dim3(wanted < kStreamGrid ? wanted : kStreamGrid), dim3(kStreamWaves * 64), 0, s>>>(a);
-        if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
-        attend_join<Core><<<dim3(a.T * a.n_units), dim3(256), 0, s>>>(a);
-    }
+    attend_item<Core><<<dim3(a.T * a.n_units), dim3(Core::kItemWaves * 64), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 
-template <template <int, bool> class Core>
-int launch_dim(const AttendArgs &a, bool one_launch, int bound, hipStream_t s)
+template <typename Core>
+int launch_stream(const AttendArgs &a, hipStream_t s)
 {
-    if (a.D == 64) return launch_core<Core<64, true>>(a, one_launch, bound, s);
-    if (a.D == 128) return launch_core<Core<128, true>>(a, one_launch, bound, s);
-    if (a.D == 256) return launch_core<Core<256, true>>(a, one_launch, bound, s);
-    if (a.D < 64) return launch_core<Core<64, false>>(a, one_launch, bound, s);
-    if (a.D < 128) return launch_core<Core<128, false>>(a, one_launch, bound, s);
-    return launch_core<Core<256, false>>(a, one_launch, bound, s);
+    typedef typename Core::Elem Elem;
+    const int pairs = a.T * a.n_units, tiles = (a.max_len + Core::kTile - 1) / Core::kTile;
+    const size_t lds = (2 * (size_t)a.T + 1) * sizeof(int);          // at most 32 KiB
+    const int64_t wanted = ((int64_t)pairs * tiles + kTeam * a.least - 1) / (kTeam * a.least);
+    attend_stream<Core><<<dim3(wanted < kStreamGrid ? (int)wanted : kStreamGrid), dim3(kTeam * 64), lds, s>>>(a);
+    if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
+    if (pairs < 256)
+        attend_join<Elem, Core::kTile, 8><<<dim3(pairs, (a.rows * (a.D / 4) + 31) / 32), dim3(256), 0, s>>>(a);
+    else
+        attend_join<Elem, Core::kTile, 1><<<dim3(pairs), dim3(256), 0, s>>>(a);
+    return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
+}
+
+template <template <int, bool, int> class Core, int DP, bool EXACT>
+int launch_cut(const AttendArgs &a, hipStream_t s)
+{
+    typedef typename Core<DP, EXACT, 0>::Elem Elem;
+    const int64_t most = (int64_t)a.T * a.pool.n_kv * a.max_len * a.D * 2 * sizeof(Elem);       // bytes, as far as the host knows
+    const bool one_launch = a.max_len <= 1024;
+    if (most > (256 << 20))
+        return one_launch ? launch_item<Core<DP, EXACT, kPassBoth>>(a, s) : launch_stream<Core<DP, EXACT, kPassBoth>>(a, s);
+    if (!one_launch) return launch_stream<Core<DP, EXACT, kPassValues>>(a, s);
+    return most > (64 << 20) ? launch_item<Core<DP, EXACT, kPassValues>>(a, s) : launch_item<Core<DP, EXACT, kKeepAll>>(a, s);
+}
+
+template <template <int, bool, int> class Core>
+int launch_dim(const AttendArgs &a, hipStream_t s)
+{
+    if (a.D == 64) return launch_cut<Core, 64, true>(a, s);
+    if (a.D == 128) return launch_cut<Core, 128, true>(a, s);
+    if (a.D == 256) return launch_cut<Core, 256, true>(a, s);
+    if (a.D < 64) return launch_cut<Core, 64, false>(a, s);
+    if (a.D < 128) return launch_cut<Core, 128, false>(a, s);
+    return launch_cut<Core, 256, false>(a, s);
 }
 
 }  // namespace
@@ -745,7 +828,7 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     if (const int rc = check_paged_shape(shape)) return rc;
     if (!q || !k_pages || !v_pages || !page_table || !lens || !out) return HALO_ERR_NULL;
     const halo_paged_shape &s = *shape;
-    const int size = s.dtype == HALO_F32 ? 4 : 2, tile = s.dtype == HALO_F32 ? 16 : 32;
+    const int size = s.dtype == HALO_F32 ? 4 : 2;
     auto odd = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; };
     if (T < 0 || T > kMaxSeqs || max_len < 1 || max_len > s.max_pages * s.page_size || !std::isfinite(scale)) return HALO_ERR_ARG;
     if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q) || odd(k_pages) || odd(v_pages) || odd(out) ||
@@ -770,9 +853,7 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.D = s.head_dim; a.max_pages = s.max_pages; a.max_len = max_len;
     a.scale2 = scale * 1.44269504088896341f;
     a.least = 4;
-    const int64_t tiles = (max_len + tile - 1) / tile, bound = tiles * T * a.n_units;
-    if (bound > (1 << 30)) return HALO_ERR_ARG;
-    const bool one_launch = max_len <= 1024;
+    if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return s.dtype == HALO_F32 ? launch_dim<CoreF32>(a, one_launch, (int)bound, st) : launch_dim<CoreBf16>(a, one_launch, (int)bound, st);
+    return s.dtype == HALO_F32 ? launch_dim<CoreF32>(a, st) : launch_dim<CoreBf16>(a, st);
 }

@@ -31,17 +31,43 @@ HALO_HOST_DEVICE int64_t paged_row(const PagePool &p, int page, int head, int po
 HALO_HOST_DEVICE int paged_length(int len, int max_len) { return len < 0 ? 0 : len < max_len ? len : max_len; }
 
 // Split attention.  The tiles of all (sequence, unit) pairs that have work stand in one line, sequence by sequence, each pair's tiles in
-// order; worker w (a wave) takes the tiles [w * per, (w + 1) * per) of it.  A pair whose tiles all fall to one worker is written out by it.
-// Of any other pair every worker keeps a partial result, in slot 0 of the worker if the pair is the first in its share, in slot 1 if not
-// (then it is the share's last): a worker never has more than these two.
+// order; worker w (a wave) takes the tiles [w * per, (w + 1) * per) of it.  kTeam consecutive workers are a workgroup.  A pair whose tiles all
+// fall to one worker is written out by it.  Of any other pair each worker has a part: its share ends inside the pair (or with it), or goes on after it.
+// Parts of the first kind meet at the end of a workgroup, which joins those of one pair; if they are all of the pair, it is written out there.
+// What is left is at most two partial results a worker: slot 2w + 1 for the joined ones, where w is the first of the workers joined, and
+// slot 2w for a share that goes on.
+constexpr int kTeam = 4;
+
 HALO_HOST_DEVICE int tiles_per_worker(int total, int workers, int least)
 {
     const int even = total / workers + (total % workers != 0);
     return even > least ? even : least;
 }
-HALO_HOST_DEVICE int first_worker(int offset, int per) { return offset / per; }
-HALO_HOST_DEVICE int last_worker(int offset, int tiles, int per) { return (offset + tiles - 1) / per; }
-// slot of worker w's partial result of the pair that begins at `offset`
-HALO_HOST_DEVICE int64_t partial_slot(int w, int per, int offset) { return 2 * (int64_t)w + ((int64_t)w * per >= offset ? 0 : 1); }
+
+// A pair's tiles [offset, offset + tiles), tiles > 0, of a line of `total` cut into shares of `per`.
+struct Cut {
+    int w0, w1;                                      // its first and last worker
+    int last;                                        // the last one whose share ends inside it: w1 or w1 - 1
+    bool whole, in_team;                             // all with one worker; all with workers of one workgroup that end inside it
+
+    HALO_HOST_DEVICE Cut(int offset, int tiles, int per, int total)
+    {
+        const int end = offset + tiles;
+        w0 = offset / per;
+        w1 = (end - 1) / per;
+        const int64_t share_end = (int64_t)(w1 + 1) * per;
+        last = (share_end < total ? share_end : total) <= end ? w1 : w1 - 1;
+        whole = w0 == w1;
+        in_team = last == w1 && w0 / kTeam == w1 / kTeam;
+    }
+    // partial results of a pair that is neither whole nor in_team, in order
+    HALO_HOST_DEVICE int parts() const { return last / kTeam - w0 / kTeam + 1 + (last < w1); }
+    HALO_HOST_DEVICE int64_t slot(int part) const
+    {
+        const int team = w0 / kTeam + part;
+        if (team > last / kTeam) return 2 * (int64_t)w1;
+        return 2 * (int64_t)(part == 0 ? w0 : team * kTeam) + 1;
+    }
+};
 
 }  // namespace halo

@@ -11,7 +11,7 @@
 
 using namespace halo;
 
-// Walks every worker's share as the first launch does and every pair as the second does; both have to agree.
+// Walks every workgroup's shares as the first launch does and every pair as the second does; both have to agree.
 static const char *check_cut(int workers, int least, const std::vector<int> &tiles)
 {
     int total = 0;
@@ -22,37 +22,59 @@ static const char *check_cut(int workers, int least, const std::vector<int> &til
     }
     const int per = tiles_per_worker(total, workers, least);
     if (per < least || (int64_t)per * workers < total) return "share";
-    std::map<std::pair<int, size_t>, int64_t> slots;             // (worker, pair) -> slot
-    std::map<int64_t, int> used;
-    std::vector<int> seen(tiles.size(), 0), whole(tiles.size(), 0);
-    for (int w = 0; w < workers; ++w) {
-        const int64_t from = (int64_t)w * per;
-        if (from >= total) break;
-        const int to = from + per < total ? (int)from + per : total;
-        for (size_t i = 0; i < tiles.size(); ++i) {
-            const int b = from > offset[i] ? (int)from : offset[i], e = to < offset[i] + tiles[i] ? to : offset[i] + tiles[i];
-            if (b >= e) continue;
-            seen[i] += e - b;
-            if (e - b == tiles[i]) {
-                whole[i] = 1;
-                continue;
+    std::map<int64_t, size_t> slots;                             // slot -> pair
+    std::vector<int> seen(tiles.size(), 0), out(tiles.size(), 0);
+    for (int team = 0; team * kTeam < workers; ++team) {
+        int key[kTeam], got[kTeam];
+        for (int i = 0; i < kTeam; ++i) {
+            const int w = team * kTeam + i;
+            key[i] = -1;
+            const int64_t from = (int64_t)w * per;
+            if (w >= workers || from >= total) continue;
+            const int to = from + per < total ? (int)from + per : total;
+            for (size_t p = 0; p < tiles.size(); ++p) {
+                const int b = from > offset[p] ? (int)from : offset[p], e = to < offset[p] + tiles[p] ? to : offset[p] + tiles[p];
+                if (b >= e) continue;
+                seen[p] += e - b;
+                if (e - b == tiles[p]) {
+                    out[p]++;
+                } else if (e < to) {                             // goes on
+                    if (slots.count(2 * w)) return "slot";
+                    slots[2 * w] = p;
+                } else {
+                    key[i] = (int)p;
+                    got[i] = e - b;
+                }
             }
-            const int64_t s = partial_slot(w, per, offset[i]);
-            if (s < 0 || s >= 2 * (int64_t)workers || used[s]++) return "slot";
-            slots[{w, i}] = s;
+        }
+        for (int i = 0; i < kTeam; ++i) {
+            if (key[i] < 0 || (i && key[i - 1] == key[i])) continue;
+            int have = 0;
+            for (int j = i; j < kTeam && key[j] == key[i]; ++j) have += got[j];
+            if (have == tiles[key[i]]) {
+                out[key[i]]++;
+            } else {
+                if (slots.count(2 * (team * kTeam + i) + 1)) return "slot";
+                slots[2 * (team * kTeam + i) + 1] = key[i];
+            }
         }
     }
-    for (size_t i = 0; i < tiles.size(); ++i) {
-        if (seen[i] != tiles[i]) return "cover";
-        if (tiles[i] == 0) continue;
-        const int w0 = first_worker(offset[i], per), w1 = last_worker(offset[i], tiles[i], per);
-        if ((w0 == w1) != (whole[i] != 0)) return "whole";
-        if (w0 == w1) continue;
-        size_t mine = 0;
-        for (const auto &kv : slots) mine += kv.first.second == i;
-        if (mine != (size_t)(w1 - w0 + 1)) return "count";
-        for (int w = w0; w <= w1; ++w)
-            if (!slots.count({w, i}) || slots[{w, i}] != partial_slot(w, per, offset[i])) return "join";
+    for (size_t p = 0; p < tiles.size(); ++p) {
+        if (seen[p] != tiles[p]) return "cover";
+        if (tiles[p] == 0) continue;
+        const Cut c(offset[p], tiles[p], per, total);
+        int mine = 0;
+        for (const auto &s : slots) mine += s.second == p;
+        if (out[p] != (c.whole || c.in_team)) return "out";
+        if (out[p]) {
+            if (mine) return "both";
+            continue;
+        }
+        if (mine != c.parts()) return "count";
+        for (int k = 0; k < c.parts(); ++k) {
+            if (c.slot(k) >= 2 * (int64_t)workers || !slots.count(c.slot(k)) || slots[c.slot(k)] != p) return "join";
+            if (k && c.slot(k) <= c.slot(k - 1)) return "order";
+        }
     }
     return "ok";
 }
