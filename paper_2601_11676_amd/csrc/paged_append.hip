@@ -1,8 +1,11 @@
 // New tokens' queries and keys rotated by their positions, keys and values written to the pages of their sequences (halo_paged_append).
 //     (a, b) -> (a cos - b sin, b cos + a sin)
-// Moves each element once and reads a token's angles once: bytes bound it, and with few tokens the launch and two round trips (position, page; then
-// the store).  A workgroup takes a token, or some of its heads where there are few tokens.  A thread keeps one place in the head -- two
-// pieces of eight elements that hold whole pairs -- and walks over the heads with it, so that its eight angles are read once.
+// Moves each element once: bytes bound it, and with few tokens the launch and two round trips (position and page; then
+// the rows).  A workgroup takes a token, or as many of its heads as have room in it; a thread takes two pieces of 16 bytes of a head that hold whole pairs,
+// so that neighbouring threads' pieces are neighbours in memory, loaded and stored as runs of half a head.  (Two pieces of eight elements whatever their
+// type, walking over the heads with a token's angles in registers, left holes between a float head's stores: 394 MB 100 us, now 68.)
+// PASS: stores with the non-temporal hint, where they fill whole 64-byte parts of lines and are many: 208 MB 41 -> 36 us (5.8 TB/s, a copy of 8 GiB
+// reaches 4.8), 112 MB of float 21.9 -> 18.3; runs of 80 bytes (heads of 80, bf16) 12.3 -> 15.5, so these do without it.
 #include "../../include/halo.h"
 
 #include <cmath>
@@ -28,13 +31,39 @@ struct AppendArgs {
     int n_heads, D, max_pages, n_seq, max_pos, rotary, pairs;
 };
 
-template <typename T>
+// 16 bytes of a head
+template <typename T> struct Piece {
+    static constexpr int kElems = 16 / sizeof(T);
+    u32x4 v;
+    __device__ __forceinline__ void get(float (&o)[kElems]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            unpack8(v, o);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(v[i]);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&x)[kElems])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2)
+                v[i] = (uint32_t)f32_to_bf16(x[2 * i]) | ((uint32_t)f32_to_bf16(x[2 * i + 1]) << 16);
+            else
+                v[i] = __float_as_uint(x[i]);
+        }
+    }
+};
+
+template <typename T, bool PASS>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
-    const int token = blockIdx.x, places = a.D / 16, heads_at_once = kAppendThreads / places;
-    const int place = threadIdx.x % places, first = threadIdx.x / places + blockIdx.y * heads_at_once;
-    const int rows = (a.q ? a.n_heads : 0) + 2 * a.pool.n_kv, k_from = a.q ? a.n_heads : 0, v_from = k_from + a.pool.n_kv;
-    if ((int)threadIdx.x >= heads_at_once * places) return;
+    constexpr int E = Piece<T>::kElems;
+    const int token = blockIdx.x, places = a.D / (2 * E), heads_at_once = kAppendThreads / places;
+    const int place = threadIdx.x % places, row = threadIdx.x / places + blockIdx.y * heads_at_once;
+    const int k_from = a.q ? a.n_heads : 0, v_from = k_from + a.pool.n_kv, rows = v_from + a.pool.n_kv;
+    if ((int)threadIdx.x >= heads_at_once * places || row >= rows) return;
 
     const int seq = a.seq ? a.seq[token] : token, pos = a.pos[token];
     int page = -1;
@@ -42,56 +71,65 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
         page = a.table[(int64_t)seq * a.max_pages + (pos >> a.pool.page_shift)];
     const bool there = page_exists(a.pool, page);    // else padding
 
-    // the two pieces of this place: a pair's elements face each other in them, or follow one another
-    const bool turned = a.rope && place * 16 < a.rotary, facing = turned && !a.pairs;
-    const int e0 = facing ? place * 8 : place * 16, e1 = facing ? place * 8 + a.rotary / 2 : place * 16 + 8;
-    float cs[8], sn[8];
-    if (turned && there) {
-        const float *angles = a.rope + (int64_t)pos * a.rotary + place * 8;
-        load8(angles, cs);
-        load8(angles + a.rotary / 2, sn);
+    // The two pieces of this place.  Elements that face each other in their pairs: place p < rotary / (2 E) has p and the piece that faces it, the other places
+    // share the rest of the head like this; else, and for values, piece p of either half of the head.
+    const bool query = row < k_from, value = row >= v_from, facing = a.rope && !a.pairs && !value;
+    const int from = facing ? a.rotary : 0, p = facing ? place - a.rotary / (2 * E) : place;
+    const bool faced = facing && p < 0;
+    const int e0 = faced ? place * E : from + p * E, e1 = faced ? e0 + a.rotary / 2 : e0 + (a.D - from) / 2;
+
+    const T *row_in;
+    T *row_out;
+    if (query) {
+        row_in = static_cast<const T *>(a.q) + token * a.q_stride + row * a.D;
+        row_out = static_cast<T *>(a.q_out) + ((int64_t)token * a.n_heads + row) * a.D;
+    } else {
+        const int head = row - (value ? v_from : k_from);
+        row_in = static_cast<const T *>(value ? a.v : a.k) + token * (value ? a.v_stride : a.k_stride) + head * a.D;
+        if (!there) return;
+        row_out = static_cast<T *>(value ? a.v_pages : a.k_pages) + paged_row(a.pool, page, head, pos) * a.D;
     }
-    for (int row = first; row < rows; row += heads_at_once * gridDim.y) {
-        const T *from;
-        T *to;
-        if (row < k_from) {
-            from = static_cast<const T *>(a.q) + token * a.q_stride + row * a.D;
-            to = static_cast<T *>(a.q_out) + ((int64_t)token * a.n_heads + row) * a.D;
-        } else {
-            const bool key = row < v_from;
-            const int head = row - (key ? k_from : v_from);
-            from = static_cast<const T *>(key ? a.k : a.v) + token * (key ? a.k_stride : a.v_stride) + head * a.D;
-            if (!there) continue;
-            to = static_cast<T *>(key ? a.k_pages : a.v_pages) + paged_row(a.pool, page, head, pos) * a.D;
-        }
-        Piece8<T> p0, p1;
-        p0.load(from + e0);
-        p1.load(from + e1);
-        if (!there) {
-            p0.zero();
-            p1.zero();
-        }
-        float x[8], y[8];
+    Piece<T> p0, p1;
+    p0.v = *reinterpret_cast<const u32x4 *>(row_in + e0);
+    p1.v = *reinterpret_cast<const u32x4 *>(row_in + e1);
+    if (!there) {
+        p0.v = p1.v = u32x4{0u, 0u, 0u, 0u};
+    } else if (faced) {
+        const float *angles = a.rope + (int64_t)pos * a.rotary + e0;
+        float x[E], y[E], u[E], w[E];
         p0.get(x);
         p1.get(y);
-        if (turned && there && row < v_from) {
-            float u[8], w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // pair i of this place: (x[i], y[i]) facing, else elements 2i and 2i + 1 of x followed by y
-                const float p = facing ? x[i] : i < 4 ? x[(2 * i) & 7] : y[(2 * i) & 7];
-                const float q = facing ? y[i] : i < 4 ? x[(2 * i + 1) & 7] : y[(2 * i + 1) & 7];
-                u[i] = p * cs[i] - q * sn[i];
-                w[i] = q * cs[i] + p * sn[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = facing ? u[i] : i & 1 ? w[i / 2] : u[i / 2];
-                y[i] = facing ? w[i] : i & 1 ? w[4 + i / 2] : u[4 + i / 2];
-            }
+        for (int i = 0; i < E; ++i) {
+            const float cs = angles[i], sn = angles[i + a.rotary / 2];
+            u[i] = x[i] * cs - y[i] * sn;
+            w[i] = y[i] * cs + x[i] * sn;
         }
-        store8(to + e0, x);
-        store8(to + e1, y);
+        p0.set(u);
+        p1.set(w);
+    } else if (a.rope && a.pairs && !value) {
+        auto turn = [&](Piece<T> &piece, int e) {
+            if (e >= a.rotary) return;
+            const float *angles = a.rope + (int64_t)pos * a.rotary + e / 2;
+            float x[E], u[E];
+            piece.get(x);
+#pragma unroll
+            for (int i = 0; i < E; i += 2) {
+                const float cs = angles[i / 2], sn = angles[i / 2 + a.rotary / 2];
+                u[i] = x[i] * cs - x[i + 1] * sn;
+                u[i + 1] = x[i + 1] * cs + x[i] * sn;
+            }
+            piece.set(u);
+        };
+        turn(p0, e0);
+        turn(p1, e1);
+    }
+    if constexpr (PASS) {
+        __builtin_nontemporal_store(p0.v, reinterpret_cast<u32x4 *>(row_out + e0));
+        __builtin_nontemporal_store(p1.v, reinterpret_cast<u32x4 *>(row_out + e1));
+    } else {
+        *reinterpret_cast<u32x4 *>(row_out + e0) = p0.v;
+        *reinterpret_cast<u32x4 *>(row_out + e1) = p1.v;
     }
 }
 
@@ -145,12 +183,18 @@ extern "C" int halo_paged_append(const halo_paged_shape *shape, int32_t N, const
     if (rope && rope_len < a.max_pos) a.max_pos = rope_len;
     a.rotary = rope ? rotary_dim : 0;
     a.pairs = rope_pairs != 0;
-    const int at_once = kAppendThreads / (s.head_dim / 16), rows = (q ? s.n_heads : 0) + 2 * s.n_kv_heads;
-    const int parts = N < 512 ? (rows + at_once - 1) / at_once : 1;
+    const int at_once = kAppendThreads / (s.head_dim * size / 32), rows = (q ? s.n_heads : 0) + 2 * s.n_kv_heads;
+    const int faced = rope && !rope_pairs ? rotary_dim : 0;
+    const bool runs = (faced / 2 * size | (s.head_dim - faced) / 2 * size | s.head_dim / 2 * size) % 64 == 0;
+    const bool pass = runs && (int64_t)N * rows * s.head_dim * size >= (4 << 20);
+    const dim3 grid(N, (rows + at_once - 1) / at_once), threads(kAppendThreads);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (s.dtype == HALO_F32)
-        append_kernel<float><<<dim3(N, parts), dim3(kAppendThreads), 0, st>>>(a);
-    else
-        append_kernel<bf16_t><<<dim3(N, parts), dim3(kAppendThreads), 0, st>>>(a);
+    if (s.dtype == HALO_F32) {
+        if (pass) append_kernel<float, true><<<grid, threads, 0, st>>>(a);
+        else append_kernel<float, false><<<grid, threads, 0, st>>>(a);
+    } else {
+        if (pass) append_kernel<bf16_t, true><<<grid, threads, 0, st>>>(a);
+        else append_kernel<bf16_t, false><<<grid, threads, 0, st>>>(a);
+    }
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
