@@ -48,7 +48,6 @@ struct AttendArgs {
     PagePool pool;
     int T, n_heads, group, n_qt, n_units, rows, D, max_pages, max_len;
     float scale2;                                    // scale * log2(e): the softmax is computed in powers of two
-    int least;                                       // tiles that a worker takes at least
 };
 
 __device__ __forceinline__ float xor_max16_32(float v)
@@ -120,6 +119,7 @@ struct CoreBf16 {
     static constexpr int kSub = DP > 64 ? 2 : 4, kTile = kSub * 16;      // rows of 128 and 64: 16 KiB of keys and values a step
     static constexpr int kItemWaves = DP > 128 ? 4 : 8;     // waves of a workgroup that takes a pair: rows of 256 need more than 256 registers
     static constexpr int kWaves = DP > 128 ? 1 : 2;         // on a SIMD, for the same reason
+    static constexpr int kSteps = DP > 64 ? 8 : 4, kLeast = DP > 128 ? 4 : 2;     // see launch_cut; tiles a worker takes at least
     static constexpr int kStage = kTile * DP * 2, kMostRows = kCols * DP * 4;    // LDS of a wave: a step's keys, in the end its part of the results
     static constexpr int KS = DP / 32;               // pieces of a key row in a lane
     static constexpr int VEC = DP > 64 ? 8 : 4, VH = DP > 128 ? 2 : 1, kAcc = VEC * VH;
@@ -229,6 +229,7 @@ template <int DP, bool EXACT, int HINT>
 struct CoreF32 {
     typedef float Elem;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
+    static constexpr int kSteps = 4, kLeast = DP > 128 ? 4 : 2;
     static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
     static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
 
@@ -595,7 +596,7 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
     line_up<Core::kTile>(a, s_base, s_len, s_wave);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto base = [&](int t) { return __builtin_amdgcn_readfirstlane(s_base[t]); };
-    const int total = base(a.T), per = tiles_per_worker(total, gridDim.x * kTeam, a.least);
+    const int total = base(a.T), per = tiles_per_worker(total, gridDim.x * kTeam, Core::kLeast);
     if (blockIdx.x == 0) {                           // for the second launch
         for (int t = threadIdx.x; t < a.T; t += kTeam * 64) a.plan[2 + t] = s_base[t];
         if (threadIdx.x == 0) a.plan[0] = per, a.plan[1] = total;
@@ -765,7 +766,7 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
     typedef typename Core::Elem Elem;
     const int pairs = a.T * a.n_units, tiles = (a.max_len + Core::kTile - 1) / Core::kTile;
     const size_t lds = (2 * (size_t)a.T + 1) * sizeof(int);          // at most 32 KiB
-    const int64_t wanted = ((int64_t)pairs * tiles + kTeam * a.least - 1) / (kTeam * a.least);
+    const int64_t wanted = ((int64_t)pairs * tiles + kTeam * Core::kLeast - 1) / (kTeam * Core::kLeast);
     attend_stream<Core><<<dim3(wanted < kStreamGrid ? (int)wanted : kStreamGrid), dim3(kTeam * 64), lds, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (pairs < 256)
@@ -775,12 +776,18 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 
+// One launch, a workgroup a pair, or even shares and a second launch: the latter costs some 5 us more, the former is as slow as its longest pair on one compute unit.
+// One launch up to kSteps steps of a wave at the longest length, twice as many where there are pairs for every unit to have two.  us, one launch / two:
+// bf16 heads of 128, 8 cache heads, 1 sequence of 1024 8.6 / 12.0, 2048 (8 steps) 12.5 / 12.2, 4096 23 / 13; 16 sequences 2048 22.3 / 26.7, 4096 44.4 / 42.9; 64
+// sequences 2048 66.5 / 73.4, 4096 134 / 134.  Float heads of 64, 1 sequence of 512 9.0 / 12.1, 1024 (4 steps) 13.8 / 12.2; 64 sequences 2048 69.9 / 75.2.
 template <template <int, bool, int> class Core, int DP, bool EXACT>
 int launch_cut(const AttendArgs &a, hipStream_t s)
 {
-    typedef typename Core<DP, EXACT, 0>::Elem Elem;
+    typedef Core<DP, EXACT, kKeepAll> C;
+    typedef typename C::Elem Elem;
     const int64_t most = (int64_t)a.T * a.pool.n_kv * a.max_len * a.D * 2 * sizeof(Elem);       // bytes, as far as the host knows
-    const bool one_launch = a.max_len <= 1024;
+    const int steps = C::kSteps * (a.T * a.n_units >= 512 ? 2 : 1);
+    const bool one_launch = a.max_len <= steps * C::kItemWaves * C::kTile;
     if (most > (256 << 20))
         return one_launch ? launch_item<Core<DP, EXACT, kPassBoth>>(a, s) : launch_stream<Core<DP, EXACT, kPassBoth>>(a, s);
     if (!one_launch) return launch_stream<Core<DP, EXACT, kPassValues>>(a, s);
@@ -852,7 +859,6 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.rows = a.group < kCols ? a.group : kCols;
     a.D = s.head_dim; a.max_pages = s.max_pages; a.max_len = max_len;
     a.scale2 = scale * 1.44269504088896341f;
-    a.least = 4;
     if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return s.dtype == HALO_F32 ? launch_dim<CoreF32>(a, st) : launch_dim<CoreBf16>(a, st);

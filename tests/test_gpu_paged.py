@@ -219,7 +219,9 @@ ATTENDS = [
     ("bf16", 40, 2, 64, 16, [1500, 700, 33], 0.5), ("bf16", 20, 1, 256, 256, [1100, 64], 0.7), ("f32", 2, 1, 240, 16, [1100, 900], None),
     ("bf16", 2, 2, 80, 16, [1600] * 3, None), ("bf16", 1, 1, 128, 4096, [9000], None), ("f32", 6, 6, 112, 16, [1030, 2, 1500], 0.5),
     ("bf16", 16, 2, 64, 16, [50 + 37 * i for i in range(70)], 0.5), ("f32", 1, 1, 16, 16, [6000], None),
-    ("bf16", 130, 130, 32, 16, [1100, 40], 0.3),
+    ("bf16", 130, 130, 32, 16, [1100, 40], 0.3), ("bf16", 130, 130, 32, 16, [2100, 40], 0.3), ("bf16", 2, 2, 80, 16, [2600] * 3, None),
+    ("bf16", 40, 2, 64, 16, [2500, 700, 33], 0.5), ("bf16", 8, 2, 128, 128, [2048, 2047], None), ("bf16", 8, 2, 128, 128, [2049, 1], None),
+    ("f32", 24, 8, 96, 16, [600] * 10, 0.6), ("bf16", 64, 64, 48, 16, [300 * i for i in range(9)], 0.5),
 ]
 
 
@@ -261,7 +263,7 @@ def test_lengths_out_of_bounds_and_pages_that_are_none(dtype, longest):
     check_attend(case, run_attend(case, max_len=longest - 3), max_len=longest - 3)
 
 
-@pytest.mark.parametrize("longest", [700, 1900])
+@pytest.mark.parametrize("longest", [700, 1900, 2500])
 def test_nan_stays_in_its_query(longest):
     # queries of NaN beside good ones of the same cache head, masked or not: the others' results keep their bits
     case = list(attend_case("bf16", 8, 2, 128, 16, [longest, 50], seed=6))
@@ -279,7 +281,7 @@ def test_nan_stays_in_its_query(longest):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("longest", [300, 2000])
+@pytest.mark.parametrize("longest", [300, 2000, 4100])
 def test_far_apart_scores(dtype, longest):
     # one key far above, then far below the rest, scores of several hundred: the maximum moves in any step
     case = attend_case(dtype, 4, 4, 64, 16, [longest, longest - 20, 100], seed=7, garbage=False)
@@ -323,23 +325,24 @@ def test_attention_repeats_its_bits_on_any_stream(longest):
 def test_a_larger_bound_or_workspace_changes_no_length():
     # max_len only bounds: both ways of cutting agree with the oracle for the same short sequences
     case = attend_case("bf16", 8, 2, 64, 16, [60, 300, 7], seed=11, extra=200)
-    for m in (300, 1000, 1025, 3000):
+    for m in (300, 1000, 1025, 2048, 2049, 3000):
         check_attend(case, run_attend(case, max_len=m))
 
 
 def test_many_sequences():
     case = attend_case("bf16", 2, 1, 16, 16, [(i * 7) % 40 for i in range(4096)], keep=0.8, seed=12)
     check_attend(case, run_attend(case))
-    case = attend_case("bf16", 2, 1, 16, 16, [(i * 7) % 40 for i in range(4095)] + [1500], keep=0.8, seed=12)
-    check_attend(case, run_attend(case))
+    for last in (1500, 9000):
+        case = attend_case("bf16", 2, 1, 16, 16, [(i * 7) % 40 for i in range(4095)] + [last], keep=0.8, seed=12)
+        check_attend(case, run_attend(case))
 
 
-@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
-def test_pools_past_32_bits(dtype, D):
+@pytest.mark.parametrize("dtype,D,longest", [("bf16", 128, 1500), ("bf16", 128, 2300), ("f32", 64, 1500), ("f32", 64, 500)])
+def test_pools_past_32_bits(dtype, D, longest):
     # the sequences' pages lie beyond 2^32 bytes and 2^31 elements of the pools, of which only they are ever written
     page, Hk = 256, 8
     n_pages = (1 << 31) // (page * Hk * D) + 40
-    small = list(attend_case(dtype, 16, Hk, D, page, [1500, 300], seed=13, garbage=False))
+    small = list(attend_case(dtype, 16, Hk, D, page, [longest, 300], seed=13, garbage=False))
     shape, q, kp, vp, table, lens, _ = small
     big = H.PagedShape(16, Hk, D, page, n_pages, shape.max_pages, dtype)
     far = torch.where(table >= 0, table + n_pages - shape.n_pages, table)
@@ -347,13 +350,13 @@ def test_pools_past_32_bits(dtype, D):
     for p, s in zip(pools, (kp, vp)):
         p[n_pages - shape.n_pages:] = s.to(DEV)
     ws = torch.empty(H.halo_paged_workspace_bytes(big, 2), dtype=torch.uint8, device=DEV)
-    rope = torch.from_numpy(H.halo_rope_table(2000, D)).to(DEV)
+    rope = torch.from_numpy(H.halo_rope_table(3000, D)).to(DEV)
     k, v = (normal(gen(i), (2, Hk, D), dtype) for i in (1, 2))
     for pool, sh, tab in ((pools, big, far), ([kp.to(DEV), vp.to(DEV)], shape, table)):
         out = torch.empty(q.shape, dtype=q.dtype, device=DEV)
         q_rot = torch.empty_like(out)
         H.halo_paged_append(sh, q.to(DEV), k.to(DEV), v.to(DEV), (lens - 1).to(DEV), tab.to(DEV), *pool, q_out=q_rot, rope=rope)
-        H.halo_paged_attention(sh, q_rot, *pool, tab.to(DEV), lens.to(DEV), 1500, out, ws)
+        H.halo_paged_attention(sh, q_rot, *pool, tab.to(DEV), lens.to(DEV), longest, out, ws)
         torch.cuda.synchronize()
         if sh is big:
             first = out, q_rot, pool[0][n_pages - shape.n_pages:].clone(), pool[1][n_pages - shape.n_pages:].clone()
@@ -424,7 +427,7 @@ def test_step_in_a_graph():
     """append -> attention -> norm of a batch, captured once: every replay, with lengths and positions moved on between them, has the bits of
     the same calls made directly."""
     T, Hq, Hk, D, page, d = 5, 8, 2, 64, 16, 512
-    case = attend_case("bf16", Hq, Hk, D, page, [1000, 40, 15, 1, 300], seed=20, garbage=False, extra=3)
+    case = attend_case("bf16", Hq, Hk, D, page, [1000, 40, 15, 1, 300], seed=20, garbage=False, extra=70)
     shape, q, kp, vp, table, lens, _ = [None if t is None else t.to(DEV) if isinstance(t, torch.Tensor) else t for t in case]
     k, v = (normal(gen(i), (T, Hk, D), "bf16").to(DEV) for i in (1, 2))
     rope = torch.from_numpy(H.halo_rope_table(2000, D)).to(DEV)
@@ -434,7 +437,7 @@ def test_step_in_a_graph():
     w = torch.randn(d, device=DEV).to(torch.bfloat16)
     q_rot, out = torch.empty_like(q), torch.empty_like(q)
     h, x = torch.empty_like(h0), torch.empty((T, d), dtype=torch.bfloat16, device=DEV)
-    for max_len in (1024, 1040):                                      # one launch, two
+    for max_len in (1024, 2060):                                      # one launch, two
         def step():
             H.halo_paged_append(shape, q, k, v, pos, table, kp, vp, q_out=q_rot, rope=rope)
             H.halo_paged_attention(shape, q_rot, kp, vp, table, lens, max_len, out, ws)

@@ -1,8 +1,10 @@
 """Serving a batch over a paged cache, without a GPU: where tokens lie and how the work is cut (the kernels' own integer arithmetic, built
 for the host), what the entry points refuse, the rotation table, and the oracle's definitions against plain numpy."""
 import ctypes as C
+import json
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -131,6 +133,48 @@ def test_binding_refuses_what_the_library_cannot_see():
         H.halo_paged_attention(s, x, x, x, i, i, 16, x, x)
     with pytest.raises(ValueError):
         H.halo_block_norm(torch.zeros(2, 64), torch.zeros(2, 64), torch.zeros(2, 64))
+
+
+# ---------------------------------------------------------------- what is launched
+LAUNCHES = """
+import ctypes as C, json, sys
+recorder = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+recorder.recorder_take.restype = C.c_char_p
+lib = C.CDLL(sys.argv[2])
+lib.halo_paged_workspace_bytes.restype = C.c_size_t
+p, out = C.c_void_p(1 << 30), []
+for heads, kv, dim, dtype, T, max_len, mask in json.load(sys.stdin):
+    shape = C.byref((C.c_int32 * 7)(heads, kv, dim, 16, 1000, max(1, (max_len + 15) // 16), dtype))
+    ws = lib.halo_paged_workspace_bytes(shape, T)
+    rc = lib.halo_paged_attention(shape, T, p, C.c_int64(heads * dim), p, p, p, p, max_len, p if mask else None, C.c_float(1.0), p, p,
+                                  C.c_size_t(ws), None)
+    out.append((rc, [l.split() for l in recorder.recorder_take().decode().split("\\n")[:-1]]))
+json.dump(out, sys.stdout)
+"""
+
+
+def _launches(calls, tmp_path):
+    shim = str(tmp_path / "recorder.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", shim, os.path.join(HERE, "launch_recorder.c")], check=True)
+    p = subprocess.run([sys.executable, "-c", LAUNCHES, shim, H.library_path()], input=json.dumps(calls), capture_output=True, text=True,
+                       timeout=120)
+    assert p.returncode == 0, p.stderr
+    return json.loads(p.stdout)
+
+
+def test_attention_launches(tmp_path):
+    # (heads, cache heads, dim, dtype, sequences, longest, mask) -> kernels and workgroups
+    cases = [((32, 8, 128, 1, 1, 2048, 0), [("attend_item", 8, 512)]), ((32, 8, 128, 1, 1, 2049, 0), [("attend_stream", 65, 256), ("attend_join", 8, 256)]),
+             ((32, 8, 128, 1, 64, 4096, 1), [("attend_item", 512, 512)]), ((32, 8, 128, 1, 64, 4097, 1), [("attend_stream", 512, 256), ("attend_join", 512, 256)]),
+             ((20, 1, 64, 1, 3, 2048, 0), [("attend_item", 6, 512)]), ((12, 4, 64, 0, 5, 1024, 0), [("attend_item", 20, 512)]),
+             ((12, 4, 64, 0, 5, 1025, 0), [("attend_stream", 83, 256), ("attend_join", 20, 256)]), ((8, 8, 256, 1, 1, 1024, 0), [("attend_item", 8, 256)]),
+             ((8, 8, 256, 0, 1, 257, 0), [("attend_stream", 9, 256), ("attend_join", 8, 256)]), ((256, 256, 16, 1, 4096, 4096, 1), [("attend_item", 1 << 20, 512)]),
+             ((256, 256, 16, 1, 4096, 9000, 1), [("attend_stream", 512, 256), ("attend_join", 1 << 20, 256)]), ((8, 8, 64, 1, 0, 64, 0), [])]
+    for (call, want), (rc, got) in zip(cases, _launches([c for c, _ in cases], tmp_path)):
+        assert rc == 0, call
+        assert len(got) == len(want), (call, got)
+        for (name, x, *_, threads), (n, grid, block) in zip(got, want):
+            assert n in name and int(x) == grid and int(threads) == block, (call, got)
 
 
 # ---------------------------------------------------------------- rotation table
