@@ -60,6 +60,7 @@ class PagedShape:
         self.c = _CPagedShape(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, code)
         self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
         self.pool = (n_pages, n_kv_heads, page_size, head_dim)       # shape of k_pages and of v_pages
+        self.pool_elems = n_pages * n_kv_heads * page_size * head_dim
 
 
 class Shape:
@@ -417,14 +418,21 @@ def _heads(t: torch.Tensor, heads: int, dim: int, dtype):
     return t.data_ptr(), apart if size[0] > 1 else heads * dim, size[0]
 
 
-def _typed(t: torch.Tensor, dtype, shape):
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{list(shape)} of {dtype} expected")
+def _dense(t: torch.Tensor, dtype, n: int):
+    """Address of n elements."""
+    if t.dtype is not dtype or t.numel() != n:
+        raise ValueError(f"{n} elements of {dtype} expected")
     if not t.is_cuda:
         raise ValueError("device tensor expected")
     if not t.is_contiguous():
         raise ValueError("contiguous tensor expected")
     return t.data_ptr()
+
+
+def _pool(t: torch.Tensor, shape: PagedShape):
+    if t.shape != shape.pool:
+        raise ValueError(f"pages are {list(shape.pool)}")
+    return _dense(t, shape.torch_dtype, shape.pool_elems)
 
 
 def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
@@ -440,18 +448,18 @@ def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pa
     if Nv != N or Nq != N:
         raise ValueError("q, k and v must hold the same tokens")
     if q_out is not None:
-        po = _typed(q_out, dt, (N, shape.n_heads, dim))
+        po = _dense(q_out, dt, N * shape.n_heads * dim)
     n_seq = page_table.shape[0]
     if seq is None and n_seq < N:
         raise ValueError("without seq, every token needs a row of the page table")
     pr, rows, half = None, 0, 0
     if rope is not None:
         rows, _, half = rope.shape
-        pr = _typed(rope, torch.float32, (rows, 2, half))
+        pr = _dense(rope, torch.float32, rows * 2 * half)
     rc = load_library().halo_paged_append(
-        shape.c, N, pq, sq, pk, sk, pv, sv, _typed(pos, torch.int32, (N,)), None if seq is None else _typed(seq, torch.int32, (N,)),
-        n_seq, _typed(page_table, torch.int32, (n_seq, shape.max_pages)), pr, rows, 2 * half, 1 if rope_pairs else 0, po,
-        _typed(k_pages, dt, shape.pool), _typed(v_pages, dt, shape.pool), _stream(stream))
+        shape.c, N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N),
+        n_seq, _dense(page_table, torch.int32, n_seq * shape.max_pages), pr, rows, 2 * half, 1 if rope_pairs else 0, po,
+        _pool(k_pages, shape), _pool(v_pages, shape), _stream(stream))
     if rc:
         raise HaloError("halo_paged_append", rc)
 
@@ -463,15 +471,15 @@ def halo_paged_workspace_bytes(shape: PagedShape, T: int) -> int:
 def halo_paged_attention(shape: PagedShape, q, k_pages, v_pages, page_table, lens, max_len: int, out, workspace, mask=None,
                          scale: Optional[float] = None, stream=None) -> None:
     """scale None: 1 / sqrt(head_dim)."""
-    dt, pool = shape.torch_dtype, shape.pool
+    dt = shape.torch_dtype
     pq, sq, T = _heads(q, shape.n_heads, shape.head_dim, dt)
     if scale is None:
         scale = shape.head_dim ** -0.5
     rc = load_library().halo_paged_attention(
-        shape.c, T, pq, sq, _typed(k_pages, dt, pool), _typed(v_pages, dt, pool),
-        _typed(page_table, torch.int32, (T, shape.max_pages)), _typed(lens, torch.int32, (T,)), max_len,
-        None if mask is None else _typed(mask, torch.uint8, (T, shape.n_heads)), scale,
-        _typed(out, dt, (T, shape.n_heads, shape.head_dim)), _ptr(workspace), workspace.nbytes, _stream(stream))
+        shape.c, T, pq, sq, _pool(k_pages, shape), _pool(v_pages, shape),
+        _dense(page_table, torch.int32, T * shape.max_pages), _dense(lens, torch.int32, T), max_len,
+        None if mask is None else _dense(mask, torch.uint8, T * shape.n_heads), scale,
+        _dense(out, dt, T * shape.n_heads * shape.head_dim), _ptr(workspace), workspace.nbytes, _stream(stream))
     if rc:
         raise HaloError("halo_paged_attention", rc)
 
@@ -479,16 +487,16 @@ def halo_paged_attention(shape: PagedShape, q, k_pages, v_pages, page_table, len
 def halo_block_norm(h, y, x, h_out=None, post_norm: bool = False, w_post=None, gate=None, res_scale: float = 1.0, w_pre=None,
                     eps: float = 1e-5, stream=None) -> None:
     """h [T][d] (h_out None: in place), y, x [T][d]; gate [d] or [T][d]."""
-    size, dt, ht = h.shape, y.dtype, h.dtype
-    T, d = size
+    T, d = h.shape
+    n, dt, ht = T * d, y.dtype, h.dtype
     pg, per_token = None, 0
     if gate is not None:
         per_token = 1 if gate.dim() == 2 else 0
-        pg = _typed(gate, dt, size if per_token else (d,))
+        pg = _dense(gate, dt, n if per_token else d)
     ph = _ptr(h)
     rc = load_library().halo_block_norm(
-        ph, _typed(y, dt, size), None if w_post is None else _typed(w_post, dt, (d,)), pg,
-        None if w_pre is None else _typed(w_pre, dt, (d,)), ph if h_out is None else _typed(h_out, ht, size), _typed(x, dt, size),
+        ph, _dense(y, dt, n), None if w_post is None else _dense(w_post, dt, d), pg,
+        None if w_pre is None else _dense(w_pre, dt, d), ph if h_out is None else _dense(h_out, ht, n), _dense(x, dt, n),
         T, d, _CODES.get(dt, -1), _CODES.get(ht, -1), 1 if post_norm else 0, per_token, res_scale, eps, _stream(stream))
     if rc:
         raise HaloError("halo_block_norm", rc)
