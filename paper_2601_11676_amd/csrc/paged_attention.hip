@@ -197,8 +197,9 @@ struct CoreBf16 {
         for (int j = 0; j < kAcc; ++j) acc[j] *= by;
         sum *= by;
     }
-    // The probabilities are rounded to bf16 here, and the sum is of the rounded ones: weights that add up to one, so that a row with one
-    // dominant token comes out as that token's values.
+    // A probability goes to the matrix cores as two bf16 values, what it rounds to and what is left of it: 2^-17 of it stays out, where one value would leave
+    // 2^-9, as much as the rounding of the output.  The cores have the time: 24 to 32 sequences' caches level, the shortest calls 5.9 -> 6.1 us.  The sum
+    // is of the same values, so that the weights add up to one.
     __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -206,8 +207,14 @@ struct CoreBf16 {
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int o = 0; o < 4 * kSub; o += 8) {
-            const u32x4 pf = {pair(p[o], p[o + 1]), pair(p[o + 2], p[o + 3]), pair(p[o + 4], p[o + 5]), pair(p[o + 6], p[o + 7])};
-            sum = mfma(ones, pf, sum);
+            u32x4 high, low;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float a = p[o + 2 * t], b = p[o + 2 * t + 1];
+                high[t] = pair(a, b);
+                low[t] = pair(a - bf16_lo(high[t]), b - bf16_hi(high[t]));
+            }
+            sum = mfma(ones, low, mfma(ones, high, sum));
 #pragma unroll
             for (int h = 0; h < VH; ++h)
 #pragma unroll
@@ -217,11 +224,17 @@ struct CoreBf16 {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         a[t] = __builtin_amdgcn_perm(vf[o + 2 * t + 1][h][j >> 1], vf[o + 2 * t][h][j >> 1], sel);
-                    acc[h * VEC + j] = mfma(a, pf, acc[h * VEC + j]);
+                    acc[h * VEC + j] = mfma(a, low, mfma(a, high, acc[h * VEC + j]));
                 }
         }
     }
-    __device__ __forceinline__ float total() const { return sum[0]; }
+    // The lane's query, its first token of each 16, whether it is the one to store what several lanes hold; the maximum over a query's lanes; what is left
+    // to do after the last step, and the query's sum.
+    __device__ __forceinline__ int col() const { return c; }
+    __device__ __forceinline__ int row() const { return g * 4; }
+    __device__ __forceinline__ bool stores() const { return true; }
+    __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
+    __device__ __forceinline__ float finish() { return sum[0]; }
 };
 
 // The same over float rows: every operand of the matrix instruction is one float a lane.
@@ -309,7 +322,123 @@ struct CoreF32 {
             for (int j = 0; j < kAcc; ++j)
                 acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[i], acc[j], 0, 0, 0);
     }
-    __device__ __forceinline__ float total() const { return xor_add<16>(xor_add<32>(l)); }
+    __device__ __forceinline__ int col() const { return c; }
+    __device__ __forceinline__ int row() const { return g * 4; }
+    __device__ __forceinline__ bool stores() const { return true; }
+    __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
+    __device__ __forceinline__ float finish() { return xor_add<16>(xor_add<32>(l)); }
+};
+
+// Up to four queries over float rows.  The float matrix instruction is slow enough to bound short caches (a step of 32 tokens, heads of 64: 0.85 us of
+// a SIMD), and with few queries most of its 16 columns are empty.  The one of 16 blocks of four rows and four columns does a quarter of the work
+// (5 sequences of up to 777, 4 cache heads of 64, three queries each: 12.1 -> 9.2 us; one of 1024, 8 heads 13.8 -> 10.5; 64 of 1024 36.6 -> 34.2):
+//   S^T  block (g, m) = rows 4m .. 4m+3 of the 16 tokens, this lane group's pieces of the row; the sum over g is an exchange
+//   O^T  block (g, m) = tokens 4m .. 4m+3, dimensions of the pieces 4g .. 4g+3; the sum over m waits until the end
+// where lane l = (g, m, j) = (l >> 4, l >> 2 & 3, l & 3), j its row of an operand and its column, a query, of the other and of the results.
+template <int DP, bool EXACT, int HINT>
+struct CoreF32Few {
+    typedef float Elem;
+    static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
+    static constexpr int kSteps = DP > 128 ? 8 : 6, kLeast = DP > 128 ? 4 : 2;
+    static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
+    static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
+
+    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[kAcc];
+    float m, l;
+    KeyPlace<float, DP> keys;
+    char *lds;
+    uint32_t voff[VH];
+    int D, g, quad, j;
+
+    __device__ __forceinline__ void place(int d, int lane, char *own)
+    {
+        D = EXACT ? DP : d;
+        g = lane >> 4;
+        quad = lane >> 2 & 3;
+        j = lane & 3;
+        lds = own;
+        keys.place(D, lane);
+#pragma unroll
+        for (int h = 0; h < VH; ++h) {
+            const int dim = h * 64 + (g * 4 + j) * 4;
+            voff[h] = EXACT || dim < D ? (uint32_t)(quad * 4 * D + dim) * 4 : kOutOfRange;
+        }
+    }
+    __device__ __forceinline__ void begin(const float *q, int nq)
+    {
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            qf[s] = j < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + j * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        l = 0.0f;
+        m = -INFINITY;
+    }
+    __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[i][s] = row_load<f32x4, HINT == kPassBoth ? kNt : 0>(rows[i], keys.from + s * keys.kRows * D * 4);
+    }
+    __device__ __forceinline__ void load_v(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < 4 * kSub; ++i)
+#pragma unroll
+            for (int h = 0; h < VH; ++h) vf[i][h] = row_load<f32x4, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 4);
+    }
+    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
+    {
+        turn_keys(*this);
+        f32x4 s[kSub][2];
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) s[i][0] = s[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < kSub; ++i)
+                    s[i][e & 1] = __builtin_amdgcn_mfma_f32_4x4x1f32(kf[i][k][e], qf[k][e], s[i][e & 1], 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4 * kSub; ++e) x[e] = xor_add<16>(xor_add<32>(s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]));
+    }
+    __device__ __forceinline__ void rescale(float by)
+    {
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) acc[i] *= by;
+        l *= by;
+    }
+    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < 4 * kSub; i += 4) l += (p[i] + p[i + 1]) + (p[i + 2] + p[i + 3]);
+#pragma unroll
+        for (int i = 0; i < 4 * kSub; ++i)
+#pragma unroll
+            for (int k = 0; k < kAcc; ++k)
+                acc[k] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[i][k >> 2][k & 3], p[i], acc[k], 0, 0, 0);
+    }
+    __device__ __forceinline__ int col() const { return j; }
+    __device__ __forceinline__ int row() const { return quad * 4; }
+    __device__ __forceinline__ bool stores() const { return quad == 0; }
+    __device__ __forceinline__ float top(float v) const
+    {
+        auto as_f = [](int i) { return __builtin_bit_cast(float, i); };
+        auto other = [&](float f, auto ctrl) { return __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, f), decltype(ctrl)::value, 0xf, 0xf, true); };
+        v = fmaxf(v, as_f(other(v, std::integral_constant<int, 0x128>{})));          // row_ror:8: lane ^ 8
+        // row_half_mirror and a reversed quad: lane ^ 4
+        return fmaxf(v, as_f(other(as_f(other(v, std::integral_constant<int, 0x141>{})), std::integral_constant<int, 0x1B>{})));
+    }
+    __device__ __forceinline__ float finish()
+    {
+#pragma unroll
+        for (int k = 0; k < kAcc; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[k][r] = xor_add<8>(xor_add<4>(acc[k][r]));
+        return xor_add<8>(xor_add<4>(l));
+    }
 };
 
 // The tiles first, first + stride, .. (count of them) of one sequence that a wave takes, and the pages of their 16-token parts: 64 parts at a time, one
@@ -369,12 +498,12 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
     for (int e = 0; e < N; ++e) x[e] *= scale2;
     if (!st.whole) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = core.g * 4 + (e & 3) < st.live[e >> 2] ? x[e] : -INFINITY;
+        for (int e = 0; e < N; ++e) x[e] = core.row() + (e & 3) < st.live[e >> 2] ? x[e] : -INFINITY;
     }
     float top = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-    top = xor_max16_32(top);
+    top = core.top(top);
     const bool passed = top > core.m + 8.0f;
     if (__ballot(passed)) {
         const float to = passed ? top : core.m;      // a query's own scores decide: its result does not depend on its neighbours
@@ -448,7 +577,7 @@ __device__ __forceinline__ void store_piece(bf16_t *p, const float (&v)[4])
 template <typename Core, typename OT>
 __device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, float by)
 {
-    if (core.c >= nq) return;
+    if (core.col() >= nq || !core.stores()) return;
 #pragma unroll
     for (int h = 0; h < Core::VH; ++h)
 #pragma unroll
@@ -457,7 +586,7 @@ __device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, f
             float v[Core::VEC];
 #pragma unroll
             for (int j = 0; j < Core::VEC; ++j) v[j] = by == 0.0f ? 0.0f : core.acc[h * Core::VEC + j][r] * by;
-            if (dim < core.D) store_piece(rows + (int64_t)core.c * core.D + dim, v);
+            if (dim < core.D) store_piece(rows + (int64_t)core.col() * core.D + dim, v);
         }
 }
 
@@ -495,15 +624,15 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
     core.place(a.D, lane, s_own + wave * Core::kStage);
     float *const s_part = reinterpret_cast<float *>(s_own);
     constexpr int kPart = Core::kStage / 4;
-    const int kept = a.mask && core.c < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + core.c] : !a.mask;
+    const int kept = a.mask && core.col() < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + core.col()] : !a.mask;
     const int len = paged_length(a.lens[t], a.max_len);
     core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
     Tiles<Core> tiles(a, t, wave, kWaves, lane);
     const int all = __ballot(kept != 0) ? (len + Core::kTile - 1) / Core::kTile : 0;
     const int count = (all - wave + kWaves - 1) / kWaves;        // all < wave: none
     if (count > 0) attend_tiles(a, core, tiles, unit.kv, len, count);
-    const float l = core.total();
-    if (core.g == 0) s_stats[wave * kCols + core.c] = make_float2(core.m, l);
+    const float l = core.finish();
+    if (core.g == 0 && core.stores()) s_stats[wave * kCols + core.col()] = make_float2(core.m, l);
     if (count > 0) store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
     __syncthreads();
     typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D;
@@ -627,20 +756,20 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
             Tiles<Core> mine(a, t, b, 1, lane);
             attend_tiles(a, core, mine, unit.kv, len, e - b);
             at = offset + e;
-            const float l = core.total();
+            const float l = core.finish();
             if (b == 0 && e == tiles) {
                 // a sum of 0 is a row without positions; NaN has to come through
-                const bool alive = core.c < unit.nq && head_alive(a, t, unit.head + core.c);
+                const bool alive = core.col() < unit.nq && head_alive(a, t, unit.head + core.col());
                 store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq,
                            !alive || l == 0.0f ? 0.0f : 1.0f / l);
             } else if (at < end) {                   // the share goes on: a partial result of its own
                 const int64_t slot = 2 * (int64_t)worker;
-                if (core.g == 0 && core.c < unit.nq)
-                    *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + core.c) * 2) = make_float2(core.m, l);
+                if (core.g == 0 && core.stores() && core.col() < unit.nq)
+                    *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + core.col()) * 2) = make_float2(core.m, l);
                 store_rows(core, a.part + slot * a.rows * core.D, unit.nq, 1.0f);
             } else {
                 last = make_int4(offset, tiles, t, units.unit());
-                if (core.g == 0) s_stats[wave * kCols + core.c] = make_float2(core.m, l);
+                if (core.g == 0 && core.stores()) s_stats[wave * kCols + core.col()] = make_float2(core.m, l);
                 store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
             }
         }
@@ -777,16 +906,19 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
 }
 
 // One launch, a workgroup a pair, or even shares and a second launch: the latter costs some 5 us more, the former is as slow as its longest pair on one compute unit.
-// One launch up to kSteps steps of a wave at the longest length, twice as many where there are pairs for every unit to have two.  us, one launch / two:
+// One launch up to kSteps steps of a wave (8; 4 and 6 where a step computes longer) at the longest length; from 512 pairs on, two for every unit, up to 8, or 16
+// with rows of 256, of which a unit has half as many waves.  us, one launch / two (lengths from half of the longest to the longest):
 // bf16 heads of 128, 8 cache heads, 1 sequence of 1024 8.6 / 12.0, 2048 (8 steps) 12.5 / 12.2, 4096 23 / 13; 16 sequences 2048 22.3 / 26.7, 4096 44.4 / 42.9; 64
-// sequences 2048 66.5 / 73.4, 4096 134 / 134.  Float heads of 64, 1 sequence of 512 9.0 / 12.1, 1024 (4 steps) 13.8 / 12.2; 64 sequences 2048 69.9 / 75.2.
+// sequences 2048 66.5 / 73.4, 4096 134 / 134, and with lengths from 0 on 127 to 131 / 125.  Heads of 64, 1 sequence of 2048 (4 steps) 12.8 / 12.5; 64 of 4000 (8) 85 / 93.
+// Heads of 256, 8 sequences of 1024 (8 steps) 17.2 / 22.1, 64 of 2048 (16) 129 / 149.  Float heads of 64, four queries a cache head, 1 sequence of 1024
+// 10.5 / 11.7, 2048 (8 steps) 16.1 / 11.8; 8 sequences 2048 15.9 / 18.7; 64 sequences 2048 65.5 / 72.2.
 template <template <int, bool, int> class Core, int DP, bool EXACT>
 int launch_cut(const AttendArgs &a, hipStream_t s)
 {
     typedef Core<DP, EXACT, kKeepAll> C;
     typedef typename C::Elem Elem;
     const int64_t most = (int64_t)a.T * a.pool.n_kv * a.max_len * a.D * 2 * sizeof(Elem);       // bytes, as far as the host knows
-    const int steps = C::kSteps * (a.T * a.n_units >= 512 ? 2 : 1);
+    const int steps = a.T * a.n_units < 512 ? C::kSteps : DP > 128 ? 16 : 8;
     const bool one_launch = a.max_len <= steps * C::kItemWaves * C::kTile;
     if (most > (256 << 20))
         return one_launch ? launch_item<Core<DP, EXACT, kPassBoth>>(a, s) : launch_stream<Core<DP, EXACT, kPassBoth>>(a, s);
@@ -861,5 +993,6 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.scale2 = scale * 1.44269504088896341f;
     if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return s.dtype == HALO_F32 ? launch_dim<CoreF32>(a, st) : launch_dim<CoreBf16>(a, st);
+    if (s.dtype == HALO_BF16) return launch_dim<CoreBf16>(a, st);
+    return a.rows <= 4 ? launch_dim<CoreF32Few>(a, st) : launch_dim<CoreF32>(a, st);
 }
