@@ -29,8 +29,8 @@ namespace halo {
 namespace {
 
 constexpr int kCols = 16;                            // queries of a unit at most: columns of the matrix instruction
-constexpr int kStreamGrid = 512;                     // workgroups of the even shares: two on each of 256 compute units
-constexpr int kMaxWorkers = kStreamGrid * kTeam;
+constexpr int kUnits = 256;                          // compute units
+constexpr int kMaxWorkers = 2 * kUnits * kTeam;      // even shares: two workgroups a unit
 constexpr int kMaxSeqs = 4096;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -47,8 +47,13 @@ struct AttendArgs {
     int64_t q_stride;
     PagePool pool;
     int T, n_heads, group, n_qt, n_units, rows, D, max_pages, max_len;
+    int64_t bytes;                                   // of the cache, for the host's choices
     float scale2;                                    // scale * log2(e): the softmax is computed in powers of two
 };
+
+// A value that is the same in every lane, said so: what descriptors are made of has to be in scalar registers (or each load becomes a loop over the lanes'
+// descriptors).
+__device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 __device__ __forceinline__ float xor_max16_32(float v)
 {
@@ -113,22 +118,23 @@ __device__ __forceinline__ void turn_keys(Core &core)
 }
 
 // The running softmax of one unit over bf16 rows, kSub times 16 tokens a step.  DP = head dimension, or the next of 64, 128, 256 above it (EXACT false).
-template <int DP, bool EXACT, int HINT>
+template <int DP, bool EXACT, int HINT, int TILES>
 struct CoreBf16 {
     typedef bf16_t Elem;
+    static constexpr int QT = TILES;                 // times 16 queries: more than one where a cache head has more than 16
     static constexpr int kSub = DP > 64 ? 2 : 4, kTile = kSub * 16;      // rows of 128 and 64: 16 KiB of keys and values a step
     static constexpr int kItemWaves = DP > 128 ? 4 : 8;     // waves of a workgroup that takes a pair: rows of 256 need more than 256 registers
-    static constexpr int kWaves = DP > 128 ? 1 : 2;         // on a SIMD, for the same reason
+    static constexpr int kWaves = DP > 128 || (DP > 64 && QT > 1) ? 1 : 2;         // on a SIMD, for the same reason
     static constexpr int kSteps = DP > 64 ? 8 : 4, kLeast = DP > 128 ? 4 : 2;     // see launch_cut; tiles a worker takes at least
-    static constexpr int kStage = kTile * DP * 2, kMostRows = kCols * DP * 4;    // LDS of a wave: a step's keys, in the end its part of the results
+    static constexpr int kMostRows = QT * kCols * DP * 4, kStage = kTile * DP * 2 > kMostRows ? kTile * DP * 2 : kMostRows;    // LDS of a wave: a step's keys, in the end its part of the results
     static constexpr int KS = DP / 32;               // pieces of a key row in a lane
     static constexpr int VEC = DP > 64 ? 8 : 4, VH = DP > 128 ? 2 : 1, kAcc = VEC * VH;
     typedef std::conditional_t<VEC == 8, u32x4, u32x2> VPiece;
 
-    u32x4 qf[KS], kf[kSub][KS];
+    u32x4 qf[QT][KS], kf[kSub][KS];
     VPiece vf[4 * kSub][VH];
-    f32x4 acc[kAcc], sum;
-    float m;
+    f32x4 acc[QT][kAcc], sum[QT];
+    float m[QT];
     KeyPlace<bf16_t, DP> keys;
     char *lds;                                       // kStage bytes, the wave's own
     uint32_t voff[VH];
@@ -150,14 +156,17 @@ struct CoreBf16 {
     __device__ __forceinline__ void begin(const bf16_t *q, int nq)
     {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int dim = s * 32 + g * 8;
-            qf[s] = c < nq && (EXACT || dim < D) ? *reinterpret_cast<const u32x4 *>(q + c * D + dim) : u32x4{0u, 0u, 0u, 0u};
-        }
+        for (int t = 0; t < QT; ++t) {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        sum = f32x4{0.f, 0.f, 0.f, 0.f};
-        m = -INFINITY;
+            for (int s = 0; s < KS; ++s) {
+                const int n = t * kCols + c, dim = s * 32 + g * 8;
+                qf[t][s] = n < nq && (EXACT || dim < D) ? *reinterpret_cast<const u32x4 *>(q + n * D + dim) : u32x4{0u, 0u, 0u, 0u};
+            }
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[t] = -INFINITY;
+        }
     }
     __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
@@ -178,43 +187,52 @@ struct CoreBf16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
     }
     // the lane's scores: 4i + r is token 16i + 4g + r of the step
-    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
+    __device__ __forceinline__ void scores(float (&x)[QT][4 * kSub])
     {
         turn_keys(*this);
-        f32x4 s[kSub];
+        f32x4 s[QT][kSub];
 #pragma unroll
-        for (int i = 0; i < kSub; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < kSub; ++i) s[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < kSub; ++i) s[i] = mfma(kf[i][k], qf[k], s[i]);
+            for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4 * kSub; ++e) x[e] = s[e >> 2][e & 3];
+                for (int i = 0; i < kSub; ++i) s[t][i] = mfma(kf[i][k], qf[t][k], s[t][i]);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4 * kSub; ++e) x[t][e] = s[t][e >> 2][e & 3];
     }
-    __device__ __forceinline__ void rescale(float by)
+    __device__ __forceinline__ void rescale(int t, float by)
     {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] *= by;
-        sum *= by;
+        for (int j = 0; j < kAcc; ++j) acc[t][j] *= by;
+        sum[t] *= by;
     }
     // A probability goes to the matrix cores as two bf16 values, what it rounds to and what is left of it: 2^-17 of it stays out, where one value would leave
     // 2^-9, as much as the rounding of the output.  The cores have the time: 24 to 32 sequences' caches level, the shortest calls 5.9 -> 6.1 us.  The sum
     // is of the same values, so that the weights add up to one.
-    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
+    __device__ __forceinline__ void accumulate(const float (&p)[QT][4 * kSub])
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
         auto pair = [](float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); };
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int o = 0; o < 4 * kSub; o += 8) {
-            u32x4 high, low;
+            u32x4 high[QT], low[QT];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float a = p[o + 2 * t], b = p[o + 2 * t + 1];
-                high[t] = pair(a, b);
-                low[t] = pair(a - bf16_lo(high[t]), b - bf16_hi(high[t]));
+            for (int q = 0; q < QT; ++q) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const float a = p[q][o + 2 * t], b = p[q][o + 2 * t + 1];
+                    high[q][t] = pair(a, b);
+                    low[q][t] = pair(a - bf16_lo(high[q][t]), b - bf16_hi(high[q][t]));
+                }
+                sum[q] = mfma(ones, low[q], mfma(ones, high[q], sum[q]));
             }
-            sum = mfma(ones, low, mfma(ones, high, sum));
 #pragma unroll
             for (int h = 0; h < VH; ++h)
 #pragma unroll
@@ -224,30 +242,39 @@ struct CoreBf16 {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         a[t] = __builtin_amdgcn_perm(vf[o + 2 * t + 1][h][j >> 1], vf[o + 2 * t][h][j >> 1], sel);
-                    acc[h * VEC + j] = mfma(a, low, mfma(a, high, acc[h * VEC + j]));
+#pragma unroll
+                    for (int q = 0; q < QT; ++q) acc[q][h * VEC + j] = mfma(a, low[q], mfma(a, high[q], acc[q][h * VEC + j]));
                 }
         }
     }
-    // The lane's query, its first token of each 16, whether it is the one to store what several lanes hold; the maximum over a query's lanes; what is left
+    // The lane's query of each 16, its first token of each 16, whether it is the one to store what several lanes hold; the maximum over a query's lanes; what is left
     // to do after the last step, and the query's sum.
     __device__ __forceinline__ int col() const { return c; }
     __device__ __forceinline__ int row() const { return g * 4; }
     __device__ __forceinline__ bool stores() const { return true; }
     __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
-    __device__ __forceinline__ float finish() { return sum[0]; }
+    __device__ __forceinline__ void finish(float (&l)[QT])
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) l[t] = sum[t][0];
+    }
 };
+
+template <int DP, bool EXACT, int HINT> using CoreBf16One = CoreBf16<DP, EXACT, HINT, 1>;
+template <int DP, bool EXACT, int HINT> using CoreBf16Two = CoreBf16<DP, EXACT, HINT, 2>;
 
 // The same over float rows: every operand of the matrix instruction is one float a lane.
 template <int DP, bool EXACT, int HINT>
 struct CoreF32 {
     typedef float Elem;
+    static constexpr int QT = 1;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
     static constexpr int kSteps = 4, kLeast = DP > 128 ? 4 : 2;
     static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
     static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
 
-    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[kAcc];
-    float m, l;
+    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[1][kAcc];
+    float m[1], l;
     KeyPlace<float, DP> keys;
     char *lds;
     uint32_t voff[VH];
@@ -272,9 +299,9 @@ struct CoreF32 {
         for (int s = 0; s < KS; ++s)
             qf[s] = c < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + c * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < kAcc; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.0f;
-        m = -INFINITY;
+        m[0] = -INFINITY;
     }
     __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
@@ -290,7 +317,7 @@ struct CoreF32 {
 #pragma unroll
             for (int h = 0; h < VH; ++h) vf[i][h] = row_load<f32x4, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 4);
     }
-    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
+    __device__ __forceinline__ void scores(float (&x)[1][4 * kSub])
     {
         turn_keys(*this);
         f32x4 s[kSub][2];
@@ -304,29 +331,29 @@ struct CoreF32 {
                 for (int i = 0; i < kSub; ++i)
                     s[i][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][k][e], qf[k][e], s[i][e & 1], 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4 * kSub; ++e) x[e] = s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3];
+        for (int e = 0; e < 4 * kSub; ++e) x[0][e] = s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3];
     }
-    __device__ __forceinline__ void rescale(float by)
+    __device__ __forceinline__ void rescale(int, float by)
     {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[j] *= by;
+        for (int j = 0; j < kAcc; ++j) acc[0][j] *= by;
         l *= by;
     }
-    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
+    __device__ __forceinline__ void accumulate(const float (&p)[1][4 * kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 4 * kSub; i += 4) l += (p[i] + p[i + 1]) + (p[i + 2] + p[i + 3]);
+        for (int i = 0; i < 4 * kSub; i += 4) l += (p[0][i] + p[0][i + 1]) + (p[0][i + 2] + p[0][i + 3]);
 #pragma unroll
         for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
             for (int j = 0; j < kAcc; ++j)
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[i], acc[j], 0, 0, 0);
+                acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[0][i], acc[0][j], 0, 0, 0);
     }
     __device__ __forceinline__ int col() const { return c; }
     __device__ __forceinline__ int row() const { return g * 4; }
     __device__ __forceinline__ bool stores() const { return true; }
     __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
-    __device__ __forceinline__ float finish() { return xor_add<16>(xor_add<32>(l)); }
+    __device__ __forceinline__ void finish(float (&out)[1]) { out[0] = xor_add<16>(xor_add<32>(l)); }
 };
 
 // Up to four queries over float rows.  The float matrix instruction is slow enough to bound short caches (a step of 32 tokens, heads of 64: 0.85 us of
@@ -338,13 +365,14 @@ struct CoreF32 {
 template <int DP, bool EXACT, int HINT>
 struct CoreF32Few {
     typedef float Elem;
+    static constexpr int QT = 1;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
     static constexpr int kSteps = DP > 128 ? 8 : 6, kLeast = DP > 128 ? 4 : 2;
     static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
     static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
 
-    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[kAcc];
-    float m, l;
+    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[1][kAcc];
+    float m[1], l;
     KeyPlace<float, DP> keys;
     char *lds;
     uint32_t voff[VH];
@@ -370,9 +398,9 @@ struct CoreF32Few {
         for (int s = 0; s < KS; ++s)
             qf[s] = j < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + j * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kAcc; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kAcc; ++i) acc[0][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.0f;
-        m = -INFINITY;
+        m[0] = -INFINITY;
     }
     __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
@@ -388,7 +416,7 @@ struct CoreF32Few {
 #pragma unroll
             for (int h = 0; h < VH; ++h) vf[i][h] = row_load<f32x4, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 4);
     }
-    __device__ __forceinline__ void scores(float (&x)[4 * kSub])
+    __device__ __forceinline__ void scores(float (&x)[1][4 * kSub])
     {
         turn_keys(*this);
         f32x4 s[kSub][2];
@@ -402,23 +430,23 @@ struct CoreF32Few {
                 for (int i = 0; i < kSub; ++i)
                     s[i][e & 1] = __builtin_amdgcn_mfma_f32_4x4x1f32(kf[i][k][e], qf[k][e], s[i][e & 1], 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4 * kSub; ++e) x[e] = xor_add<16>(xor_add<32>(s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]));
+        for (int e = 0; e < 4 * kSub; ++e) x[0][e] = xor_add<16>(xor_add<32>(s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]));
     }
-    __device__ __forceinline__ void rescale(float by)
+    __device__ __forceinline__ void rescale(int, float by)
     {
 #pragma unroll
-        for (int i = 0; i < kAcc; ++i) acc[i] *= by;
+        for (int i = 0; i < kAcc; ++i) acc[0][i] *= by;
         l *= by;
     }
-    __device__ __forceinline__ void accumulate(const float (&p)[4 * kSub])
+    __device__ __forceinline__ void accumulate(const float (&p)[1][4 * kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 4 * kSub; i += 4) l += (p[i] + p[i + 1]) + (p[i + 2] + p[i + 3]);
+        for (int i = 0; i < 4 * kSub; i += 4) l += (p[0][i] + p[0][i + 1]) + (p[0][i + 2] + p[0][i + 3]);
 #pragma unroll
         for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
             for (int k = 0; k < kAcc; ++k)
-                acc[k] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[i][k >> 2][k & 3], p[i], acc[k], 0, 0, 0);
+                acc[0][k] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[i][k >> 2][k & 3], p[0][i], acc[0][k], 0, 0, 0);
     }
     __device__ __forceinline__ int col() const { return j; }
     __device__ __forceinline__ int row() const { return quad * 4; }
@@ -431,13 +459,13 @@ struct CoreF32Few {
         // row_half_mirror and a reversed quad: lane ^ 4
         return fmaxf(v, as_f(other(as_f(other(v, std::integral_constant<int, 0x141>{})), std::integral_constant<int, 0x1B>{})));
     }
-    __device__ __forceinline__ float finish()
+    __device__ __forceinline__ void finish(float (&out)[1])
     {
 #pragma unroll
         for (int k = 0; k < kAcc; ++k)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[k][r] = xor_add<8>(xor_add<4>(acc[k][r]));
-        return xor_add<8>(xor_add<4>(l));
+            for (int r = 0; r < 4; ++r) acc[0][k][r] = xor_add<8>(xor_add<4>(acc[0][k][r]));
+        out[0] = xor_add<8>(xor_add<4>(l));
     }
 };
 
@@ -480,9 +508,10 @@ struct Step {
         for (int p = 0; p < Core::kSub; ++p) {
             const int pos = tiles.position(i) + p * 16;
             const int64_t row = paged_row(a.pool, tiles.page(i, p), kv, pos);
-            live[p] = row < 0 ? 0 : max(0, min(len - pos, 16));
+            live[p] = same(row < 0 ? 0 : max(0, min(len - pos, 16)));
             whole = whole && live[p] == 16;
-            const int64_t at = (row < 0 ? 0 : row) * a.D * kBytes;
+            const uint64_t bytes = (uint64_t)(row < 0 ? 0 : row) * (a.D * kBytes);
+            const uint64_t at = (uint64_t)(uint32_t)same((int)(bytes >> 32)) << 32 | (uint32_t)same((int)bytes);
             k[p] = buffer_of(static_cast<const char *>(a.k) + at, live[p] * a.D * kBytes);
             v[p] = buffer_of(static_cast<const char *>(a.v) + at, live[p] * a.D * kBytes);
         }
@@ -491,28 +520,32 @@ struct Step {
 
 // The part of a step between its products: scores -> probabilities, with the running maximum.  The maximum only moves when a score passes it by 8
 // (a factor of 256, which float sums take with ease), so that most steps rescale nothing.
-template <typename Core, int N>
-__device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, float scale2, float (&x)[N])
+template <typename Core>
+__device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, float scale2, float (&x)[Core::QT][4 * Core::kSub])
 {
+    constexpr int N = 4 * Core::kSub;
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] *= scale2;
-    if (!st.whole) {
+    for (int t = 0; t < Core::QT; ++t) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = core.row() + (e & 3) < st.live[e >> 2] ? x[e] : -INFINITY;
+        for (int e = 0; e < N; ++e) x[t][e] *= scale2;
+        if (!st.whole) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[t][e] = core.row() + (e & 3) < st.live[e >> 2] ? x[t][e] : -INFINITY;
+        }
+        float top = x[t][0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) top = fmaxf(top, x[t][e]);
+        top = core.top(top);
+        const bool passed = top > core.m[t] + 8.0f;
+        if (__ballot(passed)) {
+            const float to = passed ? top : core.m[t];   // a query's own scores decide: its result does not depend on its neighbours
+            core.rescale(t, to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(core.m[t] - to));
+            core.m[t] = to;
+        }
+        const float m = core.m[t] == -INFINITY ? 0.0f : core.m[t];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[t][e] = __builtin_amdgcn_exp2f(x[t][e] - m);
     }
-    float top = x[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-    top = core.top(top);
-    const bool passed = top > core.m + 8.0f;
-    if (__ballot(passed)) {
-        const float to = passed ? top : core.m;      // a query's own scores decide: its result does not depend on its neighbours
-        core.rescale(to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(core.m - to));
-        core.m = to;
-    }
-    const float m = core.m == -INFINITY ? 0.0f : core.m;
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = __builtin_amdgcn_exp2f(x[e] - m);
 }
 
 // `count` tiles of a sequence against the queries in `core`: the next step's keys are asked for as soon as this one's are used up, and its
@@ -520,7 +553,7 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
 template <typename Core>
 __device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, Tiles<Core> &tiles, int kv, int len, int count)
 {
-    float x[4 * Core::kSub];
+    float x[Core::QT][4 * Core::kSub];
     Step<Core> now(a, tiles, kv, len, 0);
     core.load_k(now.k);
     core.load_v(now.v);
@@ -540,12 +573,21 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, Ti
 
 struct Unit {
     int kv, head, nq;                                // cache head, first query head, queries
-    __device__ __forceinline__ Unit(const AttendArgs &a, int u)
+    __device__ __forceinline__ Unit(const AttendArgs &a, int u)      // u may differ from lane to lane
     {
         kv = u / a.n_qt;
-        const int from = (u - kv * a.n_qt) * kCols;
+        const int from = (u - kv * a.n_qt) * a.rows;
         head = kv * a.group + from;
-        nq = a.group - from < kCols ? a.group - from : kCols;
+        nq = min(a.group - from, a.rows);
+    }
+    static __device__ __forceinline__ Unit of_wave(const AttendArgs &a, int u) { return Unit(a, same(u)).scalars(); }
+    __device__ __forceinline__ Unit scalars() const
+    {
+        Unit r = *this;
+        r.kv = same(kv);
+        r.head = same(head);
+        r.nq = same(nq);
+        return r;
     }
 };
 
@@ -573,21 +615,39 @@ __device__ __forceinline__ void store_piece(bf16_t *p, const float (&v)[4])
                                                (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
 }
 
-// A lane's results are runs of VEC dimensions of query c: row 4g + r of instruction (h, j) is dimension h * 16 VEC + (4g + r) * VEC + j.
+// A lane's results are runs of VEC dimensions of a query: row 4g + r of instruction (h, j) is dimension h * 16 VEC + (4g + r) * VEC + j.
 template <typename Core, typename OT>
-__device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, float by)
+__device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, const float (&by)[Core::QT])
 {
-    if (core.col() >= nq || !core.stores()) return;
 #pragma unroll
-    for (int h = 0; h < Core::VH; ++h)
+    for (int t = 0; t < Core::QT; ++t) {
+        const int n = t * kCols + core.col();
+        if (n >= nq || !core.stores()) continue;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dim = h * 16 * Core::VEC + (core.g * 4 + r) * Core::VEC;
-            float v[Core::VEC];
+        for (int h = 0; h < Core::VH; ++h)
 #pragma unroll
-            for (int j = 0; j < Core::VEC; ++j) v[j] = by == 0.0f ? 0.0f : core.acc[h * Core::VEC + j][r] * by;
-            if (dim < core.D) store_piece(rows + (int64_t)core.col() * core.D + dim, v);
-        }
+            for (int r = 0; r < 4; ++r) {
+                const int dim = h * 16 * Core::VEC + (core.g * 4 + r) * Core::VEC;
+                float v[Core::VEC];
+#pragma unroll
+                for (int j = 0; j < Core::VEC; ++j) v[j] = by[t] == 0.0f ? 0.0f : core.acc[t][h * Core::VEC + j][r] * by[t];
+                if (dim < core.D) store_piece(rows + (int64_t)n * core.D + dim, v);
+            }
+    }
+}
+
+// The same as partial results, with each query's maximum and sum (l).
+template <typename Core>
+__device__ __forceinline__ void store_part(const Core &core, float *rows, float2 *stats, int nq, const float (&l)[Core::QT])
+{
+    float one[Core::QT];
+#pragma unroll
+    for (int t = 0; t < Core::QT; ++t) {
+        const int n = t * kCols + core.col();
+        one[t] = 1.0f;
+        if (core.g == 0 && core.stores() && n < nq) stats[n] = make_float2(core.m[t], l[t]);
+    }
+    store_rows(core, rows, nq, one);
 }
 
 // ---------------------------------------------------------------------------
@@ -596,15 +656,15 @@ __device__ __forceinline__ void store_rows(const Core &core, OT *rows, int nq, f
 // What the waves of a workgroup have of one pair, joined from LDS: element i of the pair's rows (query i / D) and its query's maximum and sum.
 struct Joined {
     float m, l, o;
-    __device__ __forceinline__ Joined(const float *part, int part_stride, const float2 *stats, int waves, int n, int i) : m(-INFINITY), l(0.0f), o(0.0f)
+    __device__ __forceinline__ Joined(const float *part, int part_stride, const float2 *stats, int stats_stride, int waves, int n, int i) : m(-INFINITY), l(0.0f), o(0.0f)
     {
-        for (int w = 0; w < waves; ++w) m = fmaxf(m, stats[w * kCols + n].x);
+        for (int w = 0; w < waves; ++w) m = fmaxf(m, stats[w * stats_stride + n].x);
         for (int w = 0; w < waves; ++w) {
-            const float2 ml = stats[w * kCols + n];
-            if (ml.y == 0.0f) continue;              // no positions: nothing was stored
-            const float by = __builtin_amdgcn_exp2f(ml.x - m);
+            const float2 ml = stats[w * stats_stride + n];
+            const bool none = ml.y == 0.0f;          // no positions: nothing was stored
+            const float by = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m), v = part[w * part_stride + i];
             l += ml.y * by;
-            o += part[w * part_stride + i] * by;
+            o += (none ? 0.0f : v) * by;
         }
     }
 };
@@ -615,30 +675,32 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
 {
     constexpr int kWaves = Core::kItemWaves;
     __shared__ __align__(16) char s_own[kWaves * Core::kStage];
-    __shared__ float2 s_stats[kWaves * kCols];       // maximum and sum
+    constexpr int kMost = Core::QT * kCols;
+    __shared__ float2 s_stats[kWaves * kMost];       // maximum and sum
     static_assert(Core::kStage >= Core::kMostRows, "a wave's results fit its part");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = blockIdx.x / a.n_units, u = blockIdx.x - t * a.n_units;
-    const Unit unit(a, u);
+    const int t = same(blockIdx.x / a.n_units), u = blockIdx.x - t * a.n_units;
+    const Unit unit = Unit::of_wave(a, u);
     Core core;
     core.place(a.D, lane, s_own + wave * Core::kStage);
     float *const s_part = reinterpret_cast<float *>(s_own);
     constexpr int kPart = Core::kStage / 4;
-    const int kept = a.mask && core.col() < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + core.col()] : !a.mask;
+    const int kept = a.mask && lane < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + lane] : !a.mask;
     const int len = paged_length(a.lens[t], a.max_len);
     core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
     Tiles<Core> tiles(a, t, wave, kWaves, lane);
     const int all = __ballot(kept != 0) ? (len + Core::kTile - 1) / Core::kTile : 0;
     const int count = (all - wave + kWaves - 1) / kWaves;        // all < wave: none
     if (count > 0) attend_tiles(a, core, tiles, unit.kv, len, count);
-    const float l = core.finish();
-    if (core.g == 0 && core.stores()) s_stats[wave * kCols + core.col()] = make_float2(core.m, l);
-    if (count > 0) store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
+    float l[Core::QT];
+    core.finish(l);
+    if (count > 0) store_part(core, s_part + wave * kPart, s_stats + wave * kMost, unit.nq, l);
+    else if (lane < unit.nq) s_stats[wave * kMost + lane] = make_float2(-INFINITY, 0.0f);
     __syncthreads();
     typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D;
     for (int i = threadIdx.x; i < unit.nq * core.D; i += kWaves * 64) {
         const int n = i / core.D;
-        const Joined j(s_part, kPart, s_stats, kWaves, n, i);
+        const Joined j(s_part, kPart, s_stats, kMost, kWaves, n, i);
         store_out(out + i, j.l == 0.0f || !head_alive(a, t, unit.head + n) ? 0.0f : j.o / j.l);
     }
 }
@@ -716,7 +778,8 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
 {
     __shared__ __align__(16) char s_own[kTeam * Core::kStage];
     extern __shared__ int s_line[];                  // bases [T + 1], lengths [T]
-    __shared__ float2 s_stats[kTeam * kCols];
+    constexpr int kMost = Core::QT * kCols;
+    __shared__ float2 s_stats[kTeam * kMost];
     __shared__ int s_wave[kTeam];
     __shared__ int4 s_last[kTeam];                   // the pair that a wave's share ends in: first tile (-1: none), tiles, sequence, unit
     float *const s_part = reinterpret_cast<float *>(s_own);
@@ -750,27 +813,29 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
         int n = (at - from) / tiles;
         units.find(a, t, n, lane);
         for (; at < end && at < from + size; ++n, units.next(a, t, lane)) {
-            const Unit unit(a, units.unit());
+            const Unit unit = Unit::of_wave(a, units.unit());
             const int offset = from + n * tiles, b = at - offset, e = min(tiles, end - offset);
             core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
             Tiles<Core> mine(a, t, b, 1, lane);
             attend_tiles(a, core, mine, unit.kv, len, e - b);
             at = offset + e;
-            const float l = core.finish();
+            float l[Core::QT];
+            core.finish(l);
             if (b == 0 && e == tiles) {
-                // a sum of 0 is a row without positions; NaN has to come through
-                const bool alive = core.col() < unit.nq && head_alive(a, t, unit.head + core.col());
-                store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq,
-                           !alive || l == 0.0f ? 0.0f : 1.0f / l);
+                float by[Core::QT];
+#pragma unroll
+                for (int q = 0; q < Core::QT; ++q) {
+                    const int i = q * kCols + core.col();
+                    // a sum of 0 is a row without positions; NaN has to come through
+                    by[q] = i >= unit.nq || !head_alive(a, t, unit.head + i) || l[q] == 0.0f ? 0.0f : 1.0f / l[q];
+                }
+                store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq, by);
             } else if (at < end) {                   // the share goes on: a partial result of its own
                 const int64_t slot = 2 * (int64_t)worker;
-                if (core.g == 0 && core.stores() && core.col() < unit.nq)
-                    *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + core.col()) * 2) = make_float2(core.m, l);
-                store_rows(core, a.part + slot * a.rows * core.D, unit.nq, 1.0f);
+                store_part(core, a.part + slot * a.rows * core.D, reinterpret_cast<float2 *>(a.stats) + slot * a.rows, unit.nq, l);
             } else {
                 last = make_int4(offset, tiles, t, units.unit());
-                if (core.g == 0 && core.stores()) s_stats[wave * kCols + core.col()] = make_float2(core.m, l);
-                store_rows(core, s_part + wave * kPart, unit.nq, 1.0f);
+                store_part(core, s_part + wave * kPart, s_stats + wave * kMost, unit.nq, l);
             }
         }
     }
@@ -786,7 +851,7 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
         typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)pair.z * a.n_heads + unit.head) * core.D;
         for (int i = threadIdx.x; i < unit.nq * core.D; i += kTeam * 64) {
             const int n = i / core.D;
-            const Joined j(s_part + w * kPart, kPart, s_stats + w * kCols, waves, n, i);
+            const Joined j(s_part + w * kPart, kPart, s_stats + w * kMost, kMost, waves, n, i);
             if (cut.in_team) {
                 store_out(out + i, j.l == 0.0f || !head_alive(a, pair.z, unit.head + n) ? 0.0f : j.o / j.l);
             } else {
@@ -870,11 +935,26 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
 // ---------------------------------------------------------------------------
 inline size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
+// Queries of a unit: all of a cache head up to `most`; of more, as even parts as that gives.
+inline int rows_of_unit(const halo_paged_shape &s, int most)
+{
+    const int group = s.n_heads / s.n_kv_heads, units = (group + most - 1) / most;
+    return (group + units - 1) / units;
+}
+// The most there are for any call: in bf16 and heads of up to 128 two times 16 (longer rows have no registers for it).
+inline int most_rows(const halo_paged_shape &s) { return s.dtype == HALO_BF16 && s.head_dim <= 128 ? 2 * kCols : kCols; }
+
+// Bytes of a call's cache, as far as the host knows.
+inline int64_t most_bytes(const halo_paged_shape &s, int T, int max_len)
+{
+    return (int64_t)T * s.n_kv_heads * max_len * s.head_dim * 2 * (s.dtype == HALO_F32 ? 4 : 2);
+}
+
 struct PagedWorkspace {
     size_t plan = 0, stats = 0, part = 0, bytes = 0;
     PagedWorkspace(const halo_paged_shape &s, int T)
     {
-        const size_t group = s.n_heads / s.n_kv_heads, rows = group < kCols ? group : kCols;
+        const size_t rows = rows_of_unit(s, most_rows(s));       // no call has more
         const size_t slots = 2 * (size_t)kMaxWorkers;
         stats = align256(((size_t)T + 2) * sizeof(int32_t));
         part = stats + align256(slots * rows * 2 * sizeof(float));
@@ -895,8 +975,9 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
     typedef typename Core::Elem Elem;
     const int pairs = a.T * a.n_units, tiles = (a.max_len + Core::kTile - 1) / Core::kTile;
     const size_t lds = (2 * (size_t)a.T + 1) * sizeof(int);          // at most 32 KiB
+    constexpr int grid = kUnits * Core::kWaves;                      // what is resident at once: with rows of 256 half as much
     const int64_t wanted = ((int64_t)pairs * tiles + kTeam * Core::kLeast - 1) / (kTeam * Core::kLeast);
-    attend_stream<Core><<<dim3(wanted < kStreamGrid ? (int)wanted : kStreamGrid), dim3(kTeam * 64), lds, s>>>(a);
+    attend_stream<Core><<<dim3(wanted < grid ? (int)wanted : grid), dim3(kTeam * 64), lds, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (pairs < 256)
         attend_join<Elem, Core::kTile, 8><<<dim3(pairs, (a.rows * (a.D / 4) + 31) / 32), dim3(256), 0, s>>>(a);
@@ -916,24 +997,28 @@ template <template <int, bool, int> class Core, int DP, bool EXACT>
 int launch_cut(const AttendArgs &a, hipStream_t s)
 {
     typedef Core<DP, EXACT, kKeepAll> C;
-    typedef typename C::Elem Elem;
-    const int64_t most = (int64_t)a.T * a.pool.n_kv * a.max_len * a.D * 2 * sizeof(Elem);       // bytes, as far as the host knows
     const int steps = a.T * a.n_units < 512 ? C::kSteps : DP > 128 ? 16 : 8;
     const bool one_launch = a.max_len <= steps * C::kItemWaves * C::kTile;
-    if (most > (256 << 20))
+    if (a.bytes > (256 << 20))
         return one_launch ? launch_item<Core<DP, EXACT, kPassBoth>>(a, s) : launch_stream<Core<DP, EXACT, kPassBoth>>(a, s);
     if (!one_launch) return launch_stream<Core<DP, EXACT, kPassValues>>(a, s);
-    return most > (64 << 20) ? launch_item<Core<DP, EXACT, kPassValues>>(a, s) : launch_item<Core<DP, EXACT, kKeepAll>>(a, s);
+    return a.bytes > (64 << 20) ? launch_item<Core<DP, EXACT, kPassValues>>(a, s) : launch_item<Core<DP, EXACT, kKeepAll>>(a, s);
+}
+
+template <template <int, bool, int> class Core>
+int launch_dim_128(const AttendArgs &a, hipStream_t s)
+{
+    if (a.D == 64) return launch_cut<Core, 64, true>(a, s);
+    if (a.D == 128) return launch_cut<Core, 128, true>(a, s);
+    if (a.D < 64) return launch_cut<Core, 64, false>(a, s);
+    return launch_cut<Core, 128, false>(a, s);
 }
 
 template <template <int, bool, int> class Core>
 int launch_dim(const AttendArgs &a, hipStream_t s)
 {
-    if (a.D == 64) return launch_cut<Core, 64, true>(a, s);
-    if (a.D == 128) return launch_cut<Core, 128, true>(a, s);
+    if (a.D <= 128) return launch_dim_128<Core>(a, s);
     if (a.D == 256) return launch_cut<Core, 256, true>(a, s);
-    if (a.D < 64) return launch_cut<Core, 64, false>(a, s);
-    if (a.D < 128) return launch_cut<Core, 128, false>(a, s);
     return launch_cut<Core, 256, false>(a, s);
 }
 
@@ -986,13 +1071,16 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.q_stride = q_stride;
     a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
     a.T = T; a.n_heads = s.n_heads; a.group = s.n_heads / s.n_kv_heads;
-    a.n_qt = (a.group + kCols - 1) / kCols;
+    a.bytes = most_bytes(s, T, max_len);
+    // More than 16 queries a cache head: 32 at once read the cache once, 16 at a time have more workgroups.  us, 32 / 16: 16 sequences of up to 8000, 8 cache heads
+    // with 20 queries (360 MB) 78 / 127; 30 of up to 5000, 2 with 20, heads of 96 (69 MB) 30.5 / 36.4; 8 of up to 700, 2 with 20 (4 MB) 15.7 / 11.6.
+    a.rows = rows_of_unit(s, a.bytes > (64 << 20) ? most_rows(s) : kCols);
+    a.n_qt = (a.group + a.rows - 1) / a.rows;
     a.n_units = s.n_kv_heads * a.n_qt;
-    a.rows = a.group < kCols ? a.group : kCols;
     a.D = s.head_dim; a.max_pages = s.max_pages; a.max_len = max_len;
     a.scale2 = scale * 1.44269504088896341f;
     if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (s.dtype == HALO_BF16) return launch_dim<CoreBf16>(a, st);
+    if (s.dtype == HALO_BF16) return a.rows <= kCols ? launch_dim<CoreBf16One>(a, st) : launch_dim_128<CoreBf16Two>(a, st);
     return a.rows <= 4 ? launch_dim<CoreF32Few>(a, st) : launch_dim<CoreF32>(a, st);
 }

@@ -221,6 +221,9 @@ ATTENDS = [
     ("bf16", 16, 2, 64, 16, [50 + 37 * i for i in range(70)], 0.5), ("f32", 1, 1, 16, 16, [6000], None),
     ("bf16", 130, 130, 32, 16, [1100, 40], 0.3), ("bf16", 130, 130, 32, 16, [2100, 40], 0.3), ("bf16", 2, 2, 80, 16, [2600] * 3, None),
     ("bf16", 40, 2, 64, 16, [2500, 700, 33], 0.5), ("bf16", 8, 2, 128, 128, [2048, 2047], None), ("bf16", 8, 2, 128, 128, [2049, 1], None),
+    # more than 16 queries a cache head, of caches large enough to be read once: 32 at a time
+    ("bf16", 40, 2, 128, 16, [2000, 33, 0, 1500] * 17, 0.6), ("bf16", 34, 2, 64, 32, [2500] + [7 * i for i in range(130)], 0.5),
+    ("bf16", 96, 2, 96, 16, [5000, 700] * 9, 0.3), ("bf16", 17, 1, 48, 16, [3000 + i for i in range(140)], None),
     ("f32", 24, 8, 96, 16, [600] * 10, 0.6), ("f32", 16, 4, 64, 16, SHORT + [1100], 0.7), ("f32", 5, 1, 64, 16, SHORT, None),
     ("f32", 10, 2, 128, 16, [2000, 45, 700], None), ("f32", 8, 2, 128, 32, [1700, 45, 700], 0.6), ("f32", 30, 6, 240, 16, [40, 900], None),
     ("f32", 4, 1, 32, 16, [7000, 2], None), ("f32", 6, 6, 256, 16, [700, 33], None), ("bf16", 64, 64, 48, 16, [300 * i for i in range(9)], 0.5),

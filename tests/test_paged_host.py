@@ -166,8 +166,9 @@ def test_attention_launches(tmp_path):
     # (heads, cache heads, dim, dtype, sequences, longest, mask) -> kernels and workgroups
     cases = [((32, 8, 128, 1, 1, 2048, 0), [("attend_item", 8, 512)]), ((32, 8, 128, 1, 1, 2049, 0), [("attend_stream", 65, 256), ("attend_join", 8, 256)]),
              ((32, 8, 64, 1, 64, 4096, 1), [("attend_item", 512, 512)]), ((32, 8, 64, 1, 63, 4096, 1), [("attend_stream", 512, 256), ("attend_join", 504, 256)]),
-             ((32, 8, 256, 1, 64, 2049, 1), [("attend_stream", 512, 256), ("attend_join", 512, 256)]),
-             ((20, 1, 64, 1, 3, 2048, 0), [("attend_item", 6, 512)]), ((12, 4, 64, 0, 5, 1536, 0), [("attend_item", 20, 512)]),
+             ((32, 8, 256, 1, 64, 2049, 1), [("attend_stream", 256, 256), ("attend_join", 512, 256)]),
+             ((20, 1, 64, 1, 3, 2048, 0), [("attend_item", 6, 512)]), ((40, 4, 64, 1, 64, 2048, 0), [("attend_item", 256, 512)]),
+             ((160, 8, 128, 1, 16, 8000, 0), [("attend_stream", 256, 256), ("attend_join", 128, 256)]), ((71, 1, 64, 1, 200, 5000, 0), [("attend_stream", 512, 256), ("attend_join", 600, 256)]), ((12, 4, 64, 0, 5, 1536, 0), [("attend_item", 20, 512)]),
              ((12, 4, 64, 0, 5, 1537, 0), [("attend_stream", 123, 256), ("attend_join", 20, 256)]), ((20, 4, 64, 0, 5, 1024, 0), [("attend_item", 20, 512)]),
              ((20, 4, 64, 0, 5, 1025, 0), [("attend_stream", 83, 256), ("attend_join", 20, 256)]), ((8, 8, 256, 1, 1, 1024, 0), [("attend_item", 8, 256)]),
              ((8, 8, 256, 0, 1, 513, 0), [("attend_stream", 17, 256), ("attend_join", 8, 256)]), ((256, 256, 16, 1, 4096, 4096, 1), [("attend_item", 1 << 20, 512)]),
