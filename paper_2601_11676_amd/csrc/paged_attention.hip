@@ -159,8 +159,10 @@ struct CoreBf16 {
         for (int t = 0; t < QT; ++t) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const int n = t * kCols + c, dim = s * 32 + g * 8;
-                qf[t][s] = n < nq && (EXACT || dim < D) ? *reinterpret_cast<const u32x4 *>(q + n * D + dim) : u32x4{0u, 0u, 0u, 0u};
+                // columns past the last query repeat it: nobody reads their results
+                const int n = min(t * kCols + c, nq - 1), dim = s * 32 + g * 8;
+                qf[t][s] = *reinterpret_cast<const u32x4 *>(q + n * D + (EXACT || dim < D ? dim : 0));
+                if constexpr (!EXACT) qf[t][s] = dim < D ? qf[t][s] : u32x4{0u, 0u, 0u, 0u};
             }
 #pragma unroll
             for (int j = 0; j < kAcc; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -297,7 +299,7 @@ struct CoreF32 {
     {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            qf[s] = c < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + c * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+            qf[s] = EXACT || s * 16 < D ? *reinterpret_cast<const f32x4 *>(q + min(c, nq - 1) * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < kAcc; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.0f;
@@ -396,7 +398,7 @@ struct CoreF32Few {
     {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            qf[s] = j < nq && (EXACT || s * 16 < D) ? *reinterpret_cast<const f32x4 *>(q + j * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+            qf[s] = EXACT || s * 16 < D ? *reinterpret_cast<const f32x4 *>(q + min(j, nq - 1) * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) acc[0][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.0f;
@@ -573,13 +575,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, Ti
 
 struct Unit {
     int kv, head, nq;                                // cache head, first query head, queries
-    __device__ __forceinline__ Unit(const AttendArgs &a, int u)      // u may differ from lane to lane
+    __device__ __forceinline__ Unit(const AttendArgs &a, int kv, int part) : kv(kv)
     {
-        kv = u / a.n_qt;
-        const int from = (u - kv * a.n_qt) * a.rows;
+        const int from = part * a.rows;
         head = kv * a.group + from;
         nq = min(a.group - from, a.rows);
     }
+    __device__ __forceinline__ Unit(const AttendArgs &a, int u)      // u may differ from lane to lane
+        : Unit(a, a.n_qt == 1 ? u : u / a.n_qt, a.n_qt == 1 ? 0 : u % a.n_qt) {}
     static __device__ __forceinline__ Unit of_wave(const AttendArgs &a, int u) { return Unit(a, same(u)).scalars(); }
     __device__ __forceinline__ Unit scalars() const
     {
@@ -677,19 +680,25 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
     __shared__ __align__(16) char s_own[kWaves * Core::kStage];
     constexpr int kMost = Core::QT * kCols;
     __shared__ float2 s_stats[kWaves * kMost];       // maximum and sum
+    __shared__ int s_kept[kMost];
     static_assert(Core::kStage >= Core::kMostRows, "a wave's results fit its part");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = same(blockIdx.x / a.n_units), u = blockIdx.x - t * a.n_units;
-    const Unit unit = Unit::of_wave(a, u);
+    const int t = blockIdx.z;
+    const Unit unit(a, blockIdx.x, blockIdx.y);
     Core core;
     core.place(a.D, lane, s_own + wave * Core::kStage);
     float *const s_part = reinterpret_cast<float *>(s_own);
     constexpr int kPart = Core::kStage / 4;
-    const int kept = a.mask && lane < unit.nq ? a.mask[(int64_t)t * a.n_heads + unit.head + lane] : !a.mask;
-    const int len = paged_length(a.lens[t], a.max_len);
+    // everything that tells where the rows are is asked for at once, none of it behind a condition (without a mask, any byte)
+    const uint8_t *marks = a.mask ? a.mask + (int64_t)t * a.n_heads + unit.head : reinterpret_cast<const uint8_t *>(a.lens);
+    const int mark = marks[a.mask ? min(lane, unit.nq - 1) : 0];
+    const int raw_len = a.lens[t];
     core.begin(static_cast<const typename Core::Elem *>(a.q) + t * a.q_stride + unit.head * core.D, unit.nq);
     Tiles<Core> tiles(a, t, wave, kWaves, lane);
-    const int all = __ballot(kept != 0) ? (len + Core::kTile - 1) / Core::kTile : 0;
+    const bool kept = !a.mask || mark != 0;
+    const int len = paged_length(same(raw_len), a.max_len);
+    const int all = __ballot(kept) ? (len + Core::kTile - 1) / Core::kTile : 0;
+    if (wave == 0 && lane < kMost) s_kept[lane] = kept;
     const int count = (all - wave + kWaves - 1) / kWaves;        // all < wave: none
     if (count > 0) attend_tiles(a, core, tiles, unit.kv, len, count);
     float l[Core::QT];
@@ -701,7 +710,7 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
     for (int i = threadIdx.x; i < unit.nq * core.D; i += kWaves * 64) {
         const int n = i / core.D;
         const Joined j(s_part, kPart, s_stats, kMost, kWaves, n, i);
-        store_out(out + i, j.l == 0.0f || !head_alive(a, t, unit.head + n) ? 0.0f : j.o / j.l);
+        store_out(out + i, j.l == 0.0f || !s_kept[n] ? 0.0f : j.o / j.l);
     }
 }
 
@@ -965,7 +974,7 @@ struct PagedWorkspace {
 template <typename Core>
 int launch_item(const AttendArgs &a, hipStream_t s)
 {
-    attend_item<Core><<<dim3(a.T * a.n_units), dim3(Core::kItemWaves * 64), 0, s>>>(a);
+    attend_item<Core><<<dim3(a.pool.n_kv, a.n_qt, a.T), dim3(Core::kItemWaves * 64), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 

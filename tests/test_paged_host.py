@@ -176,8 +176,9 @@ def test_attention_launches(tmp_path):
     for (call, want), (rc, got) in zip(cases, _launches([c for c, _ in cases], tmp_path)):
         assert rc == 0, call
         assert len(got) == len(want), (call, got)
-        for (name, x, *_, threads), (n, grid, block) in zip(got, want):
-            assert n in name and int(x) == grid and int(threads) == block, (call, got)
+        for (name, x, y, z, threads), (n, grid, block) in zip(got, want):
+            cut = int(y) if n == "attend_join" else 1                 # of a pair over workgroups
+            assert n in name and int(x) * int(y) * int(z) == grid * cut and int(threads) == block, (call, got)
 
 
 # ---------------------------------------------------------------- rotation table
