@@ -656,19 +656,34 @@ __device__ __forceinline__ void store_part(const Core &core, float *rows, float2
 // ---------------------------------------------------------------------------
 // one workgroup a pair
 // ---------------------------------------------------------------------------
-// What the waves of a workgroup have of one pair, joined from LDS: element i of the pair's rows (query i / D) and its query's maximum and sum.
+// What the waves of a workgroup have of one pair, joined from LDS: four dimensions of the pair's rows, the i-th four, of query n.
 struct Joined {
-    float m, l, o;
-    __device__ __forceinline__ Joined(const float *part, int part_stride, const float2 *stats, int stats_stride, int waves, int n, int i) : m(-INFINITY), l(0.0f), o(0.0f)
+    float m, l;
+    float4 o;
+    __device__ __forceinline__ Joined(const float *part, int part_stride, const float2 *stats, int stats_stride, int waves, int n, int i)
+        : m(-INFINITY), l(0.0f), o(make_float4(0.f, 0.f, 0.f, 0.f))
     {
         for (int w = 0; w < waves; ++w) m = fmaxf(m, stats[w * stats_stride + n].x);
         for (int w = 0; w < waves; ++w) {
             const float2 ml = stats[w * stats_stride + n];
             const bool none = ml.y == 0.0f;          // no positions: nothing was stored
-            const float by = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m), v = part[w * part_stride + i];
+            const float by = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+            const float4 v = *reinterpret_cast<const float4 *>(part + w * part_stride + i * 4);
             l += ml.y * by;
-            o += (none ? 0.0f : v) * by;
+            o.x += (none ? 0.0f : v.x) * by;
+            o.y += (none ? 0.0f : v.y) * by;
+            o.z += (none ? 0.0f : v.z) * by;
+            o.w += (none ? 0.0f : v.w) * by;
         }
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T *to, bool kept) const
+    {
+        // a sum of 0 is a row without positions; NaN has to come through
+        const bool none = l == 0.0f || !kept;
+        const float by = 1.0f / l;
+        const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
+        store_piece(to, v);
     }
 };
 
@@ -707,10 +722,9 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
     else if (lane < unit.nq) s_stats[wave * kMost + lane] = make_float2(-INFINITY, 0.0f);
     __syncthreads();
     typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D;
-    for (int i = threadIdx.x; i < unit.nq * core.D; i += kWaves * 64) {
-        const int n = i / core.D;
-        const Joined j(s_part, kPart, s_stats, kMost, kWaves, n, i);
-        store_out(out + i, j.l == 0.0f || !s_kept[n] ? 0.0f : j.o / j.l);
+    for (int i = threadIdx.x; i < unit.nq * (core.D / 4); i += kWaves * 64) {
+        const int n = i / (core.D / 4);
+        Joined(s_part, kPart, s_stats, kMost, kWaves, n, i).store(out + i * 4, s_kept[n]);
     }
 }
 
@@ -858,14 +872,14 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
         const Unit unit(a, pair.w);
         const int64_t slot = 2 * (int64_t)(blockIdx.x * kTeam + w) + 1;
         typename Core::Elem *out = static_cast<typename Core::Elem *>(a.out) + ((int64_t)pair.z * a.n_heads + unit.head) * core.D;
-        for (int i = threadIdx.x; i < unit.nq * core.D; i += kTeam * 64) {
-            const int n = i / core.D;
+        for (int i = threadIdx.x; i < unit.nq * (core.D / 4); i += kTeam * 64) {
+            const int n = i / (core.D / 4);
             const Joined j(s_part + w * kPart, kPart, s_stats + w * kMost, kMost, waves, n, i);
             if (cut.in_team) {
-                store_out(out + i, j.l == 0.0f || !head_alive(a, pair.z, unit.head + n) ? 0.0f : j.o / j.l);
+                j.store(out + i * 4, head_alive(a, pair.z, unit.head + n));
             } else {
-                a.part[slot * a.rows * core.D + i] = j.o;
-                if (i == n * core.D) *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + n) * 2) = make_float2(j.m, j.l);
+                *reinterpret_cast<float4 *>(a.part + slot * a.rows * core.D + i * 4) = j.o;
+                if (i == n * (core.D / 4)) *reinterpret_cast<float2 *>(a.stats + (slot * a.rows + n) * 2) = make_float2(j.m, j.l);
             }
         }
     }
@@ -884,7 +898,7 @@ __device__ __forceinline__ void take_in(float &m, float &l, float4 &o, const flo
     m = to;
 }
 
-// Joins the pairs that the first launch left in parts, and gives 0 to those that nobody had.  Workgroups (x) stand for pairs, cut by y; a thread stands
+// Joins the pairs that the first launch left in parts, and gives 0 to those that nobody had.  Workgroups stand for pairs (x, z), cut by y; a thread stands
 // for four dimensions of one query, kShares threads of a workgroup for the same, each with its share of the parts.
 template <typename Elem, int kTile, int kShares>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
@@ -893,7 +907,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
     __shared__ float4 s_o[256];
     __shared__ float2 s_ml[256];
     const int lane = threadIdx.x & 63, tid = threadIdx.x, share = tid / kQuads;
-    const int t = blockIdx.x / a.n_units, u = blockIdx.x - t * a.n_units;
+    const int t = blockIdx.z, u = blockIdx.x;
     const Unit unit(a, u);
     const int per = a.plan[0], total = a.plan[1], from = a.plan[2 + t];
     const int tiles = (paged_length(a.lens[t], a.max_len) + kTile - 1) / kTile;
@@ -913,6 +927,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
     Elem *out = static_cast<Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * a.D;
     for (int block = blockIdx.y * kQuads; block < quads; block += gridDim.y * kQuads) {
         const int i = block + tid % kQuads, n = min(i, quads - 1) / (a.D / 4);
+        const bool kept = head_alive(a, t, unit.head + n);
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i < quads)
@@ -932,8 +947,9 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
                 for (int k = 1; k < kShares; ++k) take_in(m, l, o, s_ml[k * kQuads + tid], s_o[k * kQuads + tid]);
         }
         if (share == 0 && i < quads) {
-            const bool none = l == 0.0f || !head_alive(a, t, unit.head + n);
-            const float v[4] = {none ? 0.0f : o.x / l, none ? 0.0f : o.y / l, none ? 0.0f : o.z / l, none ? 0.0f : o.w / l};
+            const bool none = l == 0.0f || !kept;
+            const float by = 1.0f / l;
+            const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
             store_piece(out + i * 4, v);
         }
     }
@@ -989,9 +1005,9 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
     attend_stream<Core><<<dim3(wanted < grid ? (int)wanted : grid), dim3(kTeam * 64), lds, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (pairs < 256)
-        attend_join<Elem, Core::kTile, 8><<<dim3(pairs, (a.rows * (a.D / 4) + 31) / 32), dim3(256), 0, s>>>(a);
+        attend_join<Elem, Core::kTile, 8><<<dim3(a.n_units, (a.rows * (a.D / 4) + 31) / 32, a.T), dim3(256), 0, s>>>(a);
     else
-        attend_join<Elem, Core::kTile, 1><<<dim3(pairs), dim3(256), 0, s>>>(a);
+        attend_join<Elem, Core::kTile, 1><<<dim3(a.n_units, 1, a.T), dim3(256), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 
