@@ -731,44 +731,98 @@ __global__ __launch_bounds__(Core::kItemWaves * 64) void attend_item(AttendArgs 
 // ---------------------------------------------------------------------------
 // even shares of all tiles
 // ---------------------------------------------------------------------------
-// s_base[t] = tiles of the sequences before t, s_base[T] = all; s_len[t] = length.  Called by the whole workgroup.
+// The line of all tiles: tiles before each sequence and its length.  Up to 64 sequences every wave has it in registers, a sequence a lane, without a mask
+// without a barrier; of more it is in LDS.  Made by the whole workgroup.
 template <int kTile>
-__device__ __forceinline__ void line_up(const AttendArgs &a, int *s_base, int *s_len, int *s_wave)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = kTeam * 64;
-    for (int t = tid; t < a.T; t += threads) {
-        s_base[t] = a.mask ? 0 : a.n_units;
-        s_len[t] = paged_length(a.lens[t], a.max_len);
-    }
-    __syncthreads();
-    if (a.mask) {
-        for (int i = tid; i < a.T * a.n_units; i += threads) {
-            const int t = i / a.n_units;
-            if (unit_alive(a, t, i - t * a.n_units)) atomicAdd(&s_base[t], 1);       // integers: any order gives the same count
-        }
-        __syncthreads();
-    }
-    const int each = (a.T + threads - 1) / threads, from = min(tid * each, a.T), to = min(from + each, a.T);
-    int mine = 0;
-    for (int t = from; t < to; ++t) {
-        const int n = s_base[t] * ((s_len[t] + kTile - 1) / kTile);
-        s_base[t] = mine;
-        mine += n;
-    }
-    int upto = mine;
+struct Line {
+    int *s_base, *s_len;                             // [T + 1], [T]
+    int before, len, T;                              // up to 64 sequences: of the lane's
+    bool small;
+
+    __device__ __forceinline__ int tiles(int n) const { return (n + kTile - 1) / kTile; }
+    static __device__ __forceinline__ int upto(int v, int lane)
+    {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(v, d);
+            if (lane >= d) v += o;
+        }
+        return v;
     }
-    if (lane == 63) s_wave[wave] = upto;
-    __syncthreads();
-    int before = upto - mine;
-    for (int w = 0; w < wave; ++w) before += s_wave[w];
-    for (int t = from; t < to; ++t) s_base[t] += before;
-    if (tid == threads - 1) s_base[a.T] = before + mine;
-    __syncthreads();
-}
+    __device__ __forceinline__ Line(const AttendArgs &a, int *s_line, int *s_wave) : s_base(s_line), s_len(s_line + a.T + 1), T(a.T), small(a.T <= 64)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = kTeam * 64;
+        if (a.mask) {
+            // the first look at the mask and the lengths are asked for together
+            const int pairs = T * a.n_units;
+            auto alive = [&](int i) {
+                const int t = i / a.n_units;
+                return unit_alive(a, t, i - t * a.n_units) ? t : -1;
+            };
+            int hit = tid < pairs ? alive(tid) : -1;
+            for (int t = tid; t < T; t += threads) {
+                s_base[t] = 0;
+                s_len[t] = paged_length(a.lens[t], a.max_len);
+            }
+            __syncthreads();
+            for (int i = tid;;) {
+                if (hit >= 0) atomicAdd(&s_base[hit], 1);        // integers: any order gives the same count
+                if ((i += threads) >= pairs) break;
+                hit = alive(i);
+            }
+            __syncthreads();
+        } else if (!small) {
+            for (int t = tid; t < T; t += threads) {
+                s_base[t] = a.n_units;
+                s_len[t] = paged_length(a.lens[t], a.max_len);
+            }
+            __syncthreads();
+        }
+        if (small) {
+            const int t = min(lane, T - 1);
+            len = a.mask ? s_len[t] : paged_length(a.lens[t], a.max_len);
+            const int mine = lane < T ? (a.mask ? s_base[t] : a.n_units) * tiles(len) : 0;
+            const int all = upto(mine, lane);
+            before = all - mine;
+            total = __builtin_amdgcn_readlane(all, 63);
+            return;
+        }
+        const int each = (T + threads - 1) / threads, from = min(tid * each, T), to = min(from + each, T);
+        int mine = 0;
+        for (int t = from; t < to; ++t) {
+            const int n = s_base[t] * tiles(s_len[t]);
+            s_base[t] = mine;
+            mine += n;
+        }
+        const int all = upto(mine, lane);
+        if (lane == 63) s_wave[wave] = all;
+        __syncthreads();
+        int others = all - mine;
+        for (int w = 0; w < wave; ++w) others += s_wave[w];
+        for (int t = from; t < to; ++t) s_base[t] += others;
+        if (tid == threads - 1) s_base[T] = others + mine;
+        __syncthreads();
+        total = same(s_base[T]);
+    }
+    int total;
+    // all wave-uniform
+    __device__ __forceinline__ int base(int t) const
+    {
+        return !small ? same(s_base[t]) : t < T ? __builtin_amdgcn_readlane(before, t) : total;
+    }
+    __device__ __forceinline__ int length(int t) const { return small ? __builtin_amdgcn_readlane(len, t) : same(s_len[t]); }
+    // the sequence whose tiles hold `at`: base(t) <= at < base(t + 1)
+    __device__ __forceinline__ int holds(int at, int lane) const
+    {
+        if (small) return __popcll(__ballot(lane < T && before <= at)) - 1;
+        int lo = 0, hi = T;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (base(mid) <= at) lo = mid; else hi = mid;
+        }
+        return lo;
+    }
+};
 
 // The surviving units of a sequence in order, 64 of them looked at at a time.
 struct AliveUnits {
@@ -807,31 +861,24 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
     __shared__ int4 s_last[kTeam];                   // the pair that a wave's share ends in: first tile (-1: none), tiles, sequence, unit
     float *const s_part = reinterpret_cast<float *>(s_own);
     constexpr int kPart = Core::kStage / 4;
-    int *const s_base = s_line, *const s_len = s_line + a.T + 1;
-    line_up<Core::kTile>(a, s_base, s_len, s_wave);
+    const Line<Core::kTile> line(a, s_line, s_wave);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    auto base = [&](int t) { return __builtin_amdgcn_readfirstlane(s_base[t]); };
-    const int total = base(a.T), per = tiles_per_worker(total, gridDim.x * kTeam, Core::kLeast);
+    const int total = line.total, per = tiles_per_worker(total, gridDim.x * kTeam, Core::kLeast);
     if (blockIdx.x == 0) {                           // for the second launch
-        for (int t = threadIdx.x; t < a.T; t += kTeam * 64) a.plan[2 + t] = s_base[t];
+        for (int t = threadIdx.x; t < a.T; t += kTeam * 64) a.plan[2 + t] = line.small ? line.before : line.s_base[t];
         if (threadIdx.x == 0) a.plan[0] = per, a.plan[1] = total;
     }
     const int worker = blockIdx.x * kTeam + wave;
     int at = (int)min((int64_t)worker * per, (int64_t)total);
     const int end = (int)min((int64_t)at + per, (int64_t)total);
-    int lo = 0, hi = a.T;                            // the sequence whose tiles hold `at`: base[lo] <= at < base[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (base(mid) <= at) lo = mid; else hi = mid;
-    }
     Core core;
     core.place(a.D, lane, s_own + wave * Core::kStage);
     AliveUnits units;
     int4 last = make_int4(-1, 0, 0, 0);
-    for (int t = lo; at < end; ++t) {
-        const int from = base(t), size = base(t + 1) - from;
+    for (int t = line.holds(at, lane); at < end; ++t) {
+        const int from = line.base(t), size = line.base(t + 1) - from;
         if (size == 0) continue;
-        const int len = __builtin_amdgcn_readfirstlane(s_len[t]);
+        const int len = line.length(t);
         const int tiles = (len + Core::kTile - 1) / Core::kTile;
         int n = (at - from) / tiles;
         units.find(a, t, n, lane);
