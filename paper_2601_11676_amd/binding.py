@@ -12,7 +12,13 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libhalo.so")
 _lib = None
-_tls = threading.local()      # prepared(): the recorder standing in for the library in this thread, if any
+
+
+class _Local(threading.local):
+    recorders = None          # prepared(): what stands in for the library in this thread, if anything
+
+
+_tls = _Local()
 
 HALO_F32, HALO_BF16 = 0, 1
 _CODES = {torch.float32: HALO_F32, torch.bfloat16: HALO_BF16}
@@ -87,7 +93,7 @@ def load_library():
     """Load libhalo.so (built in-tree by paper_2601_11676_amd.build).  There is no fallback:
     a missing library is an error."""
     global _lib
-    stack = getattr(_tls, "recorders", None)
+    stack = _tls.recorders
     if stack:
         return stack[-1]
     if _lib is not None:
@@ -526,7 +532,7 @@ def prepared(fn, *args, **kwargs):
     The recording is local to the calling thread (other threads keep calling the real library)
     and nests."""
     rec = _Recorder(load_library())
-    stack = getattr(_tls, "recorders", None)
+    stack = _tls.recorders
     if stack is None:
         stack = _tls.recorders = []
     stack.append(rec)
