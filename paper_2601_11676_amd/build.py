@@ -7,13 +7,15 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libhalo.so")
 
 FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fno-fast-math", "-Wall", "-Wextra", "-Wno-unused-parameter",
     # the first kernel arguments arrive in scalar registers with the wave instead of through a load
@@ -29,10 +31,16 @@ def sources():
 
 def build(verbose: bool = False, extra=()) -> str:
     extra = list(extra) + os.environ.get("HALO_EXTRA_FLAGS", "").split()
-    cmd = ["hipcc", *FLAGS, *extra, "-o", OUT, *sources()]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as tmp:
+        # the files side by side (each is a program of its own to the compiler), then one library of them
+        cmds = [["hipcc", *FLAGS, *extra, "-c", "-o", os.path.join(tmp, os.path.basename(s) + ".o"), s] for s in sources()]
+        link = ["hipcc", *FLAGS, *extra, "-shared", "-o", OUT, *[c[-2] for c in cmds]]
+        if verbose:
+            print("\n".join(" ".join(c) for c in (*cmds, link)), flush=True)
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            for done in [pool.submit(subprocess.run, c, check=True) for c in cmds]:
+                done.result()
+        subprocess.run(link, check=True)
     return OUT
 
 
