@@ -3,8 +3,8 @@
 // one pass over the rows with the running maximum and sum of the softmax.  Bytes bound it: a cached element meets `group` queries,
 // 4 * group / 2 operations a byte in bf16, where this card has about 200 to spare.
 //
-// A wave is the worker.  The queries of one cache head (up to 16: a unit) are the 16 columns of the matrix instruction, so that grouped heads share
-// what is read; with one query a column of 16 is used, and the matrix cores still outrun the stream.
+// A wave is the worker.  The queries of one cache head (up to 16, over large caches 32: a unit) are the columns of the matrix instruction, so that grouped heads
+// share what is read; with one query a column of 16 is used, and the matrix cores still outrun the stream.
 //   S^T = K Q^T      rows = tokens, columns = queries.  A lane (c = lane & 15, g = lane >> 4) wants pieces (16 bytes) of token c's row; loaded
 //                    like that, an instruction touches 16 rows.  So whole rows are loaded, and pass through a part of LDS that is the wave's own.
 //                    The result leaves the lane with query c's scores of the tokens 4g .. 4g+3 of each 16.
@@ -28,7 +28,7 @@
 namespace halo {
 namespace {
 
-constexpr int kCols = 16;                            // queries of a unit at most: columns of the matrix instruction
+constexpr int kCols = 16;                            // columns of the matrix instruction: queries
 constexpr int kUnits = 256;                          // compute units
 constexpr int kMaxWorkers = 2 * kUnits * kTeam;      // even shares: two workgroups a unit
 constexpr int kMaxSeqs = 4096;
@@ -82,10 +82,11 @@ __device__ __forceinline__ V row_load(__amdgpu_buffer_rsrc_t rows, uint32_t at)
 enum { kKeepAll = 0, kPassValues = 1, kPassBoth = 2 };
 
 // Keys on their way from whole rows, as they are loaded, to the lanes that multiply them: 16 rows of DP elements in LDS, piece p of row r at place
-// p ^ r (within 16), so that neither side meets a bank twice.  kRows rows a load; the same number of loads as of pieces a lane gets.
+// p ^ r (within 16), so that neither side meets a bank twice.  kRows rows a load; the same number of loads as of pieces a lane gets.  (With each lane
+// loading its pieces itself, 8 sequences of up to 1000 took 12.8 us, now 9.0.)
 template <typename Elem, int DP>
 struct KeyPlace {
-    static constexpr int kBytes = DP * sizeof(Elem), kPieces = kBytes / 16, kRows = 64 / kPieces, kLoads = kPieces / 4;
+    static constexpr int kBytes = DP * sizeof(Elem), kPieces = kBytes / 16, kRows = 64 / kPieces;
     static constexpr int kTurn = (kPieces < 16 ? kPieces : 16) - 1;
     uint32_t from, in, out;                          // offset in memory, places in LDS of the first load and of the first piece
 
@@ -737,6 +738,7 @@ template <int kTile>
 struct Line {
     int *s_base, *s_len;                             // [T + 1], [T]
     int before, len, T;                              // up to 64 sequences: of the lane's
+    int total;                                       // all tiles
     bool small;
 
     __device__ __forceinline__ int tiles(int n) const { return (n + kTile - 1) / kTile; }
@@ -804,7 +806,6 @@ struct Line {
         __syncthreads();
         total = same(s_base[T]);
     }
-    int total;
     // all wave-uniform
     __device__ __forceinline__ int base(int t) const
     {
@@ -1051,6 +1052,8 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
     const int64_t wanted = ((int64_t)pairs * tiles + kTeam * Core::kLeast - 1) / (kTeam * Core::kLeast);
     attend_stream<Core><<<dim3(wanted < grid ? (int)wanted : grid), dim3(kTeam * 64), lds, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
+    // few pairs are cut into many parts each, shared by eight threads (one sequence of 32771, 8 cache heads: 37 us by one, 5); many pairs have few
+    // parts, and then the shares cost (96 sequences, 8 cache heads: 5 us of the pass, 290 for 285 with eight)
     if (pairs < 256)
         attend_join<Elem, Core::kTile, 8><<<dim3(a.n_units, (a.rows * (a.D / 4) + 31) / 32, a.T), dim3(256), 0, s>>>(a);
     else
