@@ -227,7 +227,26 @@ ATTENDS = [
     ("f32", 24, 8, 96, 16, [600] * 10, 0.6), ("f32", 16, 4, 64, 16, SHORT + [1100], 0.7), ("f32", 5, 1, 64, 16, SHORT, None),
     ("f32", 10, 2, 128, 16, [2000, 45, 700], None), ("f32", 8, 2, 128, 32, [1700, 45, 700], 0.6), ("f32", 30, 6, 240, 16, [40, 900], None),
     ("f32", 4, 1, 32, 16, [7000, 2], None), ("f32", 6, 6, 256, 16, [700, 33], None), ("bf16", 64, 64, 48, 16, [300 * i for i in range(9)], 0.5),
+    # short caches of many sequences, and many a little longer: fewer waves a workgroup
+    ("bf16", 16, 8, 128, 16, [1 + i % 16 for i in range(70)], 0.7), ("bf16", 8, 8, 64, 32, [3 * i for i in range(80)], 0.6),
+    ("f32", 32, 8, 64, 16, [2 * i for i in range(64)], None), ("f32", 48, 4, 128, 16, [(5 * i) % 321 for i in range(130)], 0.6),
+    ("bf16", 40, 8, 80, 16, [257 + 5 * i for i in range(65)], 0.6), ("bf16", 4, 4, 256, 16, [(7 * i) % 129 for i in range(129)], 0.5),
+    ("bf16", 64, 32, 128, 16, [(11 * i) % 257 for i in range(70)], 0.5), ("f32", 4, 4, 256, 64, [20, 32, 0, 1], None),
+    ("bf16", 32, 8, 128, 16, [64, 63, 0, 1, 33], 0.5), ("bf16", 32, 8, 128, 16, [600 - i for i in range(64)], None),
+    ("bf16", 16, 16, 128, 16, [500 + i % 100 for i in range(64)], 0.8),
 ]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("seqs,longest", [(3, 30), (140, 60), (140, 200)])
+def test_rows_of_short_caches_that_the_mask_leaves_empty(dtype, seqs, longest):
+    case = attend_case(dtype, 8, 4, 64, 16, [(longest - 7 * i) % (longest + 1) for i in range(seqs)], keep=0.5, seed=9)
+    mask, lens = case[6], case[5]
+    mask[0] = 0
+    mask[1, :2], mask[1, 2:] = 0, 255
+    got = run_attend(case)
+    check_attend(case, got)
+    assert torch.all(got[0] == 0) and torch.all(got[1, :2] == 0) and torch.all(got[1, 2:] != 0) and torch.all(got.cpu()[lens.cpu() == 0] == 0)
 
 
 @pytest.mark.parametrize("args", ATTENDS, ids=lambda a: "-".join(map(str, a[:5])) + f"-{max(a[5])}x{len(a[5])}")

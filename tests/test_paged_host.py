@@ -172,7 +172,13 @@ def test_attention_launches(tmp_path):
              ((12, 4, 64, 0, 5, 1537, 0), [("attend_stream", 123, 256), ("attend_join", 20, 256)]), ((20, 4, 64, 0, 5, 1024, 0), [("attend_item", 20, 512)]),
              ((20, 4, 64, 0, 5, 1025, 0), [("attend_stream", 83, 256), ("attend_join", 20, 256)]), ((8, 8, 256, 1, 1, 1024, 0), [("attend_item", 8, 256)]),
              ((8, 8, 256, 0, 1, 513, 0), [("attend_stream", 17, 256), ("attend_join", 8, 256)]), ((256, 256, 16, 1, 4096, 4096, 1), [("attend_item", 1 << 20, 512)]),
-             ((256, 256, 16, 1, 4096, 9000, 1), [("attend_stream", 512, 256), ("attend_join", 1 << 20, 256)]), ((8, 8, 64, 1, 0, 64, 0), [])]
+             ((256, 256, 16, 1, 4096, 9000, 1), [("attend_stream", 512, 256), ("attend_join", 1 << 20, 256)]), ((8, 8, 64, 1, 0, 64, 0), []),
+             # fewer waves: up to two tiles, and of 512 pairs up to 8 and 16
+             ((32, 8, 64, 1, 1, 64, 0), [("attend_item", 8, 128)]), ((32, 8, 128, 1, 1, 65, 0), [("attend_item", 8, 512)]),
+             ((32, 8, 128, 1, 64, 256, 0), [("attend_item", 512, 128)]), ((32, 8, 128, 1, 64, 257, 0), [("attend_item", 512, 256)]),
+             ((32, 8, 128, 1, 64, 512, 0), [("attend_item", 512, 256)]), ((32, 8, 128, 1, 64, 513, 0), [("attend_item", 512, 512)]),
+             ((32, 8, 128, 1, 63, 256, 0), [("attend_item", 504, 512)]), ((16, 16, 128, 0, 32, 128, 0), [("attend_item", 512, 128)]),
+             ((16, 16, 128, 0, 32, 129, 0), [("attend_item", 512, 256)])]
     for (call, want), (rc, got) in zip(cases, _launches([c for c, _ in cases], tmp_path)):
         assert rc == 0, call
         assert len(got) == len(want), (call, got)
