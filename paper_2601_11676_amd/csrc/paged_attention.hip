@@ -30,8 +30,8 @@ inline int rows_of_unit(const halo_paged_shape &s, int most)
     const int group = s.n_heads / s.n_kv_heads, units = (group + most - 1) / most;
     return (group + units - 1) / units;
 }
-// The most there are for any call: in bf16 and heads of up to 128 two times 16 (longer rows have no registers for it).
-inline int most_rows(const halo_paged_shape &s) { return s.dtype == HALO_BF16 && s.head_dim <= 128 ? 2 * kCols : kCols; }
+// The most there are for any call: with heads of up to 128 two times 16 (longer rows have no registers for it).
+inline int most_rows(const halo_paged_shape &s) { return s.head_dim <= 128 ? 2 * kCols : kCols; }
 
 // Bytes of a call's cache, as far as the host knows.
 inline int64_t most_bytes(const halo_paged_shape &s, int T, int max_len)
@@ -105,6 +105,7 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.bytes = most_bytes(s, T, max_len);
     // More than 16 queries a cache head: 32 at once read the cache once, 16 at a time have more workgroups.  us, 32 / 16: 16 sequences of up to 8000, 8 cache heads
     // with 20 queries (360 MB) 78 / 127; 30 of up to 5000, 2 with 20, heads of 96 (69 MB) 30.5 / 36.4; 8 of up to 700, 2 with 20 (4 MB) 15.7 / 11.6.
+    // Float, 8 cache heads with 20 queries: 24 of up to 5000 135 / 228; 4 of up to 4000 (131 MB) 32.9 / 41.9; 4 of up to 1000 (32 MB) 21.5 / 21.0; 1 of 1000 19.7 / 15.0.
     a.rows = rows_of_unit(s, a.bytes > (64 << 20) ? most_rows(s) : kCols);
     a.n_qt = (a.group + a.rows - 1) / a.rows;
     a.n_units = s.n_kv_heads * a.n_qt;
@@ -113,5 +114,5 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (s.dtype == HALO_BF16) return a.rows <= kCols ? launch_attend_bf16(a, st) : launch_attend_bf16_32(a, st);
-    return a.rows <= 4 ? launch_attend_f32_4(a, st) : launch_attend_f32(a, st);
+    return a.rows <= 4 ? launch_attend_f32_4(a, st) : a.rows <= kCols ? launch_attend_f32(a, st) : launch_attend_f32_32(a, st);
 }

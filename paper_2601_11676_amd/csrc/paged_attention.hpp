@@ -250,18 +250,20 @@ struct CoreBf16 {
 template <int DP, bool EXACT, int HINT> using CoreBf16One = CoreBf16<DP, EXACT, HINT, 1>;
 template <int DP, bool EXACT, int HINT> using CoreBf16Two = CoreBf16<DP, EXACT, HINT, 2>;
 
-// The same over float rows: every operand of the matrix instruction is one float a lane.
-template <int DP, bool EXACT, int HINT>
+// The same over float rows: every operand of the matrix instruction is one float a lane.  With 32 queries and rows of 128 one wave a SIMD, which has
+// 350 registers; two with 256 each take 153 us where one takes 135 (24 sequences of up to 5000, 8 cache heads of 20 queries).
+template <int DP, bool EXACT, int HINT, int TILES>
 struct CoreF32 {
     typedef float Elem;
-    static constexpr int QT = 1;
+    static constexpr int QT = TILES;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
     static constexpr int kSteps = 4, kLeast = DP > 128 ? 4 : 2;
-    static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 ? 1 : 2, kStage = kTile * DP * 4, kMostRows = kCols * DP * 4;
+    static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 || (DP > 64 && QT > 1) ? 1 : 2;
+    static constexpr int kMostRows = QT * kCols * DP * 4, kStage = kTile * DP * 4 > kMostRows ? kTile * DP * 4 : kMostRows;
     static constexpr int KS = DP / 16, VEC = 4, VH = DP / 64, kAcc = VEC * VH;
 
-    f32x4 qf[KS], kf[kSub][KS], vf[4 * kSub][VH], acc[1][kAcc];
-    float m[1], l;
+    f32x4 qf[QT][KS], kf[kSub][KS], vf[4 * kSub][VH], acc[QT][kAcc];
+    float m[QT], l[QT];
     KeyPlace<float, DP> keys;
     char *lds;
     uint32_t voff[VH];
@@ -283,12 +285,15 @@ struct CoreF32 {
     __device__ __forceinline__ void begin(const float *q, int nq)
     {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            qf[s] = EXACT || s * 16 < D ? *reinterpret_cast<const f32x4 *>(q + min(c, nq - 1) * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < QT; ++t) {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        l = 0.0f;
-        m[0] = -INFINITY;
+            for (int s = 0; s < KS; ++s)
+                qf[t][s] = EXACT || s * 16 < D ? *reinterpret_cast<const f32x4 *>(q + min(t * kCols + c, nq - 1) * D + s * 16 + g * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            l[t] = 0.0f;
+            m[t] = -INFINITY;
+        }
     }
     __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
     {
@@ -304,44 +309,61 @@ struct CoreF32 {
 #pragma unroll
             for (int h = 0; h < VH; ++h) vf[i][h] = row_load<f32x4, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D * 4);
     }
-    __device__ __forceinline__ void scores(float (&x)[1][4 * kSub])
+    __device__ __forceinline__ void scores(float (&x)[QT][4 * kSub])
     {
         turn_keys(*this);
-        f32x4 s[kSub][2];
+        f32x4 s[QT][kSub][2];
 #pragma unroll
-        for (int i = 0; i < kSub; ++i) s[i][0] = s[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < kSub; ++i) s[t][i][0] = s[t][i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int i = 0; i < kSub; ++i)
-                    s[i][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][k][e], qf[k][e], s[i][e & 1], 0, 0, 0);
+                for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4 * kSub; ++e) x[0][e] = s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3];
+                    for (int i = 0; i < kSub; ++i)
+                        s[t][i][e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][k][e], qf[t][k][e], s[t][i][e & 1], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4 * kSub; ++e) x[t][e] = s[t][e >> 2][0][e & 3] + s[t][e >> 2][1][e & 3];
     }
-    __device__ __forceinline__ void rescale(int, float by)
+    __device__ __forceinline__ void rescale(int t, float by)
     {
 #pragma unroll
-        for (int j = 0; j < kAcc; ++j) acc[0][j] *= by;
-        l *= by;
+        for (int j = 0; j < kAcc; ++j) acc[t][j] *= by;
+        l[t] *= by;
     }
-    __device__ __forceinline__ void accumulate(const float (&p)[1][4 * kSub])
+    __device__ __forceinline__ void accumulate(const float (&p)[QT][4 * kSub])
     {
 #pragma unroll
-        for (int i = 0; i < 4 * kSub; i += 4) l += (p[0][i] + p[0][i + 1]) + (p[0][i + 2] + p[0][i + 3]);
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4 * kSub; i += 4) l[t] += (p[t][i] + p[t][i + 1]) + (p[t][i + 2] + p[t][i + 3]);
 #pragma unroll
         for (int i = 0; i < 4 * kSub; ++i)
 #pragma unroll
             for (int j = 0; j < kAcc; ++j)
-                acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[0][i], acc[0][j], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+                    acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j >> 2][j & 3], p[t][i], acc[t][j], 0, 0, 0);
     }
     __device__ __forceinline__ int col() const { return c; }
     __device__ __forceinline__ int row() const { return g * 4; }
     __device__ __forceinline__ bool stores() const { return true; }
     __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
-    __device__ __forceinline__ void finish(float (&out)[1]) { out[0] = xor_add<16>(xor_add<32>(l)); }
+    __device__ __forceinline__ void finish(float (&out)[QT])
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) out[t] = xor_add<16>(xor_add<32>(l[t]));
+    }
 };
+
+template <int DP, bool EXACT, int HINT> using CoreF32One = CoreF32<DP, EXACT, HINT, 1>;
+template <int DP, bool EXACT, int HINT> using CoreF32Two = CoreF32<DP, EXACT, HINT, 2>;
 
 // Up to four queries over float rows.  The float matrix instruction is slow enough to bound short caches (a step of 32 tokens, heads of 64: 0.85 us of
 // a SIMD), and with few queries most of its 16 columns are empty.  The one of 16 blocks of four rows and four columns does a quarter of the work
@@ -1020,7 +1042,10 @@ template <template <int, bool, int> class Core, int DP, bool EXACT, int kWaves>
 int launch_pairs(const AttendArgs &a, hipStream_t s)
 {
     if (a.bytes > (256 << 20)) return launch_item<Core<DP, EXACT, kPassBoth>, kWaves>(a, s);
-    return a.bytes > (64 << 20) ? launch_item<Core<DP, EXACT, kPassValues>, kWaves>(a, s) : launch_item<Core<DP, EXACT, kKeepAll>, kWaves>(a, s);
+    if constexpr (Core<DP, EXACT, kKeepAll>::QT == 1) {          // more queries: large caches only
+        if (a.bytes <= (64 << 20)) return launch_item<Core<DP, EXACT, kKeepAll>, kWaves>(a, s);
+    }
+    return launch_item<Core<DP, EXACT, kPassValues>, kWaves>(a, s);
 }
 
 // One launch, a workgroup a pair, or even shares and a second launch: the latter costs some 5 us more, the former is as slow as its longest pair on one compute unit.
@@ -1037,15 +1062,14 @@ int launch_cut(const AttendArgs &a, hipStream_t s)
     const bool many = a.T * a.n_units >= 512;
     const int steps = !many ? C::kSteps : DP > 128 ? 16 : 8;
     const bool one_launch = a.max_len <= steps * C::kItemWaves * C::kTile;
-    if constexpr (C::QT == 1) {
-        // Fewer waves a workgroup where more would have no tile, and where workgroups are many anyway: all of their waves wait for the slowest.
-        // us, heads of 128, 8 cache heads, by waves 8 / 4 / 2: 1 sequence of up to 64 (2 tiles) 3.9 / 3.7 / 3.6, of 128 4.1 / 4.1 / 4.6; 128 sequences of 16 10.2 / 7.0 /
-        // 4.5, of 256 (8 tiles) 21.8 / 18.4 / 18.1; 192 of 300 (10) 34.7 / 29.7 / 31.4, of 600 (19) 58.2 / 58.6 / 61.8; 32 of 128, 256 pairs, 5.1 / 5.0 / 5.2.
-        const int tiles = (a.max_len + C::kTile - 1) / C::kTile;
-        if (tiles <= 2 || (many && tiles <= 8)) return launch_pairs<Core, DP, EXACT, 2>(a, s);
-        if constexpr (C::kItemWaves > 4) {
-            if (many && tiles <= 16) return launch_pairs<Core, DP, EXACT, 4>(a, s);
-        }
+    // Fewer waves a workgroup where more would have no tile, and where workgroups are many anyway: all of their waves wait for the slowest.
+    // us, heads of 128, 8 cache heads, by waves 8 / 4 / 2: 1 sequence of up to 64 (2 tiles) 3.9 / 3.7 / 3.6, of 128 4.1 / 4.1 / 4.6; 128 sequences of 16 10.2 / 7.0 /
+    // 4.5, of 256 (8 tiles) 21.8 / 18.4 / 18.1; 192 of 300 (10) 34.7 / 29.7 / 31.4, of 600 (19) 58.2 / 58.6 / 61.8; 32 of 128, 256 pairs, 5.1 / 5.0 / 5.2.  With 20
+    // queries a cache head, 8 / 2: 200 sequences of up to 250 44.7 / 31.9, 500 of up to 60 in float 123 / 72.5; 100 of up to 500, 8 / 4, 35.7 / 36.0.
+    const int tiles = (a.max_len + C::kTile - 1) / C::kTile;
+    if (tiles <= 2 || (many && tiles <= 8)) return launch_pairs<Core, DP, EXACT, 2>(a, s);
+    if constexpr (C::kItemWaves > 4) {
+        if (many && tiles <= 16) return launch_pairs<Core, DP, EXACT, 4>(a, s);
     }
     if (one_launch) return launch_pairs<Core, DP, EXACT, C::kItemWaves>(a, s);
     return a.bytes > (256 << 20) ? launch_stream<Core<DP, EXACT, kPassBoth>>(a, s) : launch_stream<Core<DP, EXACT, kPassValues>>(a, s);
@@ -1070,11 +1094,12 @@ int launch_dim(const AttendArgs &a, hipStream_t s)
 
 }  // namespace
 
-// One for each kind of rows and queries, each in a file of its own: bf16 with up to 16 queries a cache head at once, with up to 32 (heads of up to 128),
-// float with up to 4 and up to 16.
+// One for each kind of rows and queries, each in a file of its own: bf16 with up to 16 queries a cache head at once and with up to 32 (heads of up to 128),
+// float with up to 4, 16 and 32 (heads of up to 128).
 int launch_attend_bf16(const AttendArgs &a, hipStream_t s);
 int launch_attend_bf16_32(const AttendArgs &a, hipStream_t s);
 int launch_attend_f32_4(const AttendArgs &a, hipStream_t s);
 int launch_attend_f32(const AttendArgs &a, hipStream_t s);
+int launch_attend_f32_32(const AttendArgs &a, hipStream_t s);
 
 }  // namespace halo

@@ -3,6 +3,6 @@
 
 namespace halo {
 
-int launch_attend_f32(const AttendArgs &a, hipStream_t s) { return launch_dim<CoreF32>(a, s); }
+int launch_attend_f32(const AttendArgs &a, hipStream_t s) { return launch_dim<CoreF32One>(a, s); }
 
 }  // namespace halo

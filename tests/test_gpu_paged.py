@@ -234,6 +234,13 @@ ATTENDS = [
     ("bf16", 64, 32, 128, 16, [(11 * i) % 257 for i in range(70)], 0.5), ("f32", 4, 4, 256, 64, [20, 32, 0, 1], None),
     ("bf16", 32, 8, 128, 16, [64, 63, 0, 1, 33], 0.5), ("bf16", 32, 8, 128, 16, [600 - i for i in range(64)], None),
     ("bf16", 16, 16, 128, 16, [500 + i % 100 for i in range(64)], 0.8),
+    # float with more than 16 queries a cache head, of large caches; and such queries over many short caches
+    ("f32", 40, 2, 128, 16, [2000, 33, 0, 1500] * 9, 0.6), ("f32", 34, 2, 64, 32, [2500] + [7 * i for i in range(70)], 0.5),
+    ("f32", 96, 2, 96, 16, [5000, 700] * 5, 0.3), ("f32", 17, 1, 48, 16, [1500 + i for i in range(140)], None),
+    ("f32", 160, 8, 128, 16, [(11 * i) % 129 for i in range(80)], 0.5), ("f32", 64, 2, 128, 16, [(7 * i) % 257 for i in range(260)], None),
+    ("f32", 40, 2, 96, 64, [1020 - i for i in range(50)], 0.4), ("bf16", 160, 8, 128, 16, [(11 * i) % 257 for i in range(80)], 0.5),
+    ("bf16", 66, 2, 64, 16, [(13 * i) % 513 for i in range(260)], 0.7), ("bf16", 34, 2, 80, 16, [300 + i % 200 for i in range(260)], None),
+    ("f32", 20, 1, 16, 16, [40000, 30000, 5], None),
 ]
 
 

@@ -178,7 +178,12 @@ def test_attention_launches(tmp_path):
              ((32, 8, 128, 1, 64, 256, 0), [("attend_item", 512, 128)]), ((32, 8, 128, 1, 64, 257, 0), [("attend_item", 512, 256)]),
              ((32, 8, 128, 1, 64, 512, 0), [("attend_item", 512, 256)]), ((32, 8, 128, 1, 64, 513, 0), [("attend_item", 512, 512)]),
              ((32, 8, 128, 1, 63, 256, 0), [("attend_item", 504, 512)]), ((16, 16, 128, 0, 32, 128, 0), [("attend_item", 512, 128)]),
-             ((16, 16, 128, 0, 32, 129, 0), [("attend_item", 512, 256)])]
+             ((16, 16, 128, 0, 32, 129, 0), [("attend_item", 512, 256)]),
+             # more than 16 queries a cache head: 32 at a time of caches past 64 MiB
+             ((20, 1, 128, 0, 64, 1024, 0), [("attend_stream", 512, 256), ("attend_join", 128, 256)]),
+             ((20, 1, 128, 0, 64, 1025, 0), [("attend_stream", 256, 256), ("attend_join", 64, 256)]),
+             ((20, 1, 144, 0, 64, 1025, 0), [("attend_stream", 256, 256), ("attend_join", 128, 256)]),
+             ((160, 8, 128, 0, 64, 129, 0), [("attend_item", 512, 256)]), ((160, 8, 128, 1, 64, 257, 0), [("attend_item", 512, 256)])]
     for (call, want), (rc, got) in zip(cases, _launches([c for c, _ in cases], tmp_path)):
         assert rc == 0, call
         assert len(got) == len(want), (call, got)
