@@ -418,7 +418,7 @@ int halo_paged_append(const halo_paged_shape *shape, int32_t N, const void *q, i
 /*
  * Attention of one new token of each of T sequences over its pages (its own key and value already appended):
  *   out[t][h] = sum_j p_j V_j,   p = softmax_j(scale * q[t][h] . K_j),   j over positions 0 .. lens[t]-1
- * Scores, softmax and sums are float32; with bf16 the probabilities keep 16 significant bits for the product with the values.
+ * Scores, softmax and sums are float32; with bf16 a probability enters the product with the values as three bf16 values, which hold all of its bits.
  *   q [T][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [T][n_heads][head_dim] dense
  *   page_table [T][max_pages], lens [T] int32 on the device
  *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.

@@ -199,9 +199,10 @@ struct CoreBf16 {
         for (int j = 0; j < kAcc; ++j) acc[t][j] *= by;
         sum[t] *= by;
     }
-    // A probability goes to the matrix cores as two bf16 values, what it rounds to and what is left of it: 2^-17 of it stays out, where one value would leave
-    // 2^-9, as much as the rounding of the output.  The cores have the time: 24 to 32 sequences' caches level, the shortest calls 5.9 -> 6.1 us.  The sum
-    // is of the same values, so that the weights add up to one.
+    // A probability goes to the matrix cores as three bf16 values, each what the ones before leave of it, rounded: three times eight bits are all that a float
+    // has.  The sum is of the same values, so that the weights add up to one.  (Two of
+    // them would leave up to 2^-17 of it.  us, two / three: one sequence of 301 5.1 / 5.3, 8 of up to 1000 9.5 / 9.8, heads of 256 15.1 / 16.4, 192 of up to 600
+    // 58.7 / 61.4; large caches, also with 20 queries a cache head, level: the matrix cores have the time.)
     __device__ __forceinline__ void accumulate(const float (&p)[QT][4 * kSub])
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -209,16 +210,21 @@ struct CoreBf16 {
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int o = 0; o < 4 * kSub; o += 8) {
-            u32x4 high[QT], low[QT];
+            u32x4 part[QT][3];
 #pragma unroll
             for (int q = 0; q < QT; ++q) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    const float a = p[q][o + 2 * t], b = p[q][o + 2 * t + 1];
-                    high[q][t] = pair(a, b);
-                    low[q][t] = pair(a - bf16_lo(high[q][t]), b - bf16_hi(high[q][t]));
+                    float a = p[q][o + 2 * t], b = p[q][o + 2 * t + 1];
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+                        part[q][i][t] = pair(a, b);
+                        a -= bf16_lo(part[q][i][t]);
+                        b -= bf16_hi(part[q][i][t]);
+                    }
                 }
-                sum[q] = mfma(ones, low[q], mfma(ones, high[q], sum[q]));
+#pragma unroll
+                for (int i = 0; i < 3; ++i) sum[q] = mfma(ones, part[q][i], sum[q]);
             }
 #pragma unroll
             for (int h = 0; h < VH; ++h)
@@ -230,7 +236,9 @@ struct CoreBf16 {
                     for (int t = 0; t < 4; ++t)
                         a[t] = __builtin_amdgcn_perm(vf[o + 2 * t + 1][h][j >> 1], vf[o + 2 * t][h][j >> 1], sel);
 #pragma unroll
-                    for (int q = 0; q < QT; ++q) acc[q][h * VEC + j] = mfma(a, low[q], mfma(a, high[q], acc[q][h * VEC + j]));
+                    for (int q = 0; q < QT; ++q)
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) acc[q][h * VEC + j] = mfma(a, part[q][i], acc[q][h * VEC + j]);
                 }
         }
     }

@@ -1,0 +1,89 @@
+"""Attention over a paged cache where single terms of its sums show: queries and keys that make the scores exact, values that cancel.  Against the
+oracle in double, as tests/test_gpu_paged.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_11676_amd as H
+from oracle import ref
+
+DEV = "cuda"
+F = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def paged(dtype, Hq, Hk, D, page, lens, max_len, seed=0):
+    """A call's shape, page table (scattered pages; entries past a length name a page of NaN), lengths and pools of NaN."""
+    g = torch.Generator().manual_seed(seed)
+    need = [(n + page - 1) // page for n in lens]
+    width, n_pages = (max_len + page - 1) // page, sum(need) + 1
+    ids = torch.randperm(n_pages, generator=g).to(torch.int32)
+    table = torch.full((len(lens), width), int(ids[-1]), dtype=torch.int32)
+    at = 0
+    for t, c in enumerate(need):
+        table[t, :c] = ids[at:at + c]
+        at += c
+    shape = H.PagedShape(Hq, Hk, D, page, n_pages, width, dtype)
+    pools = [torch.full(shape.pool, float("nan"), dtype=DT[dtype]) for _ in range(2)]
+    return shape, table, torch.tensor(lens, dtype=torch.int32), pools
+
+
+def put(pool, table, t, rows):
+    """rows [tokens][heads][D] to the pages of sequence t."""
+    page = pool.shape[2]
+    for i in range(0, len(rows), page):
+        part = rows[i:i + page]
+        pool[int(table[t, i // page]), :, :len(part)] = part.transpose(0, 1).to(pool.dtype)
+
+
+def attend(shape, table, lens, pools, q, max_len, scale=1.0, mask=None):
+    ws = torch.full((H.halo_paged_workspace_bytes(shape, len(lens)),), 0xff, dtype=torch.uint8, device=DEV)
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device=DEV)
+    H.halo_paged_attention(shape, q.to(DEV), pools[0].to(DEV), pools[1].to(DEV), table.to(DEV), lens.to(DEV), max_len, out, ws, scale=scale,
+                           mask=None if mask is None else mask.to(DEV))
+    torch.cuda.synchronize()
+    return out.cpu().double().numpy()
+
+
+def wanted(table, lens, pools, q, scale=1.0, mask=None):
+    return ref.paged_attention(*(x.double().numpy() for x in (q, *pools)), table.numpy(), lens.numpy(), None if mask is None else mask.numpy(), scale)
+
+
+# ---------------------------------------------------------------- probabilities
+def left_over():
+    """Scores s (bf16) of whose exp(s) two bf16 parts leave the most, with the parts and what they leave in units of the power of two below exp(s)."""
+    s = -torch.arange(1, 257, dtype=torch.float64) / 256
+    s = s.to(torch.bfloat16).double().unique()
+    r = torch.exp(s)
+    a = r.to(torch.bfloat16).double()
+    b = (r - a).to(torch.bfloat16).double()
+    left = (r - a - b) / 2.0 ** torch.floor(torch.log2(r))
+    best = left.abs().argsort(descending=True)[:8]
+    assert left[best].abs().min() >= 2.0 ** -18
+    return s[best], a[best], b[best], left[best]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hk,D,length,max_len", [
+    (8, 8, 128, 300, 300), (8, 8, 64, 50, 50), (16, 8, 96, 700, 700), (8, 8, 256, 90, 90), (8, 8, 128, 4000, 4000), (32, 8, 64, 5000, 5000),
+    (8, 8, 256, 1500, 1500), (160, 8, 128, 300, 20000), (160, 8, 64, 3000, 40000)])
+def test_probabilities_are_as_fine_as_floats(Hq, Hk, D, length, max_len):
+    # Cache head i: two tokens of score 0 with values a, b and one of score s_i with value -1, where a + b is exp(s_i) but for its last eight bits; the rest at -200
+    # counts for nothing.  The result is those bits: (a + b - r) / (2 + r).  Off by: r's exponent of s log2(e), two roundings, and its own, 2 (|s| + 1) F;
+    # six terms of the sum, each at most r, to 2 F of it (a truncating sum's); the result's rounding.
+    s, a, b, left = left_over()
+    shape, table, lens, pools = paged("bf16", Hq, Hk, D, 16, [length], max_len)
+    k, v = torch.zeros(length, Hk, D), torch.zeros(length, Hk, D)
+    k[:, :, 0] = -200.0
+    at = length // 2 // 16 * 16 + 4                                   # three tokens of one page
+    k[at:at + 2, :, 0], k[at + 2, :, 0] = 0.0, s.float()
+    v[at], v[at + 1], v[at + 2] = a.float()[:, None], b.float()[:, None], -1.0
+    put(pools[0], table, 0, k)
+    put(pools[1], table, 0, v)
+    q = torch.zeros(1, Hq, D, dtype=torch.bfloat16)
+    q[:, :, 0] = 1.0
+    got, want = attend(shape, table, lens, pools, q, max_len), wanted(table, lens, pools, q)
+    r = torch.exp(s).numpy().repeat(Hq // Hk)[None, :, None]
+    bound = r * F * (2 * (np.abs(s.numpy()).repeat(Hq // Hk)[None, :, None] + 1) + 12) / (2 + r) + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(want) > 1.5 * bound)                         # two parts alone would give 0
+    assert np.all(np.abs(got - want) <= bound), np.abs(got - want).max((0, 2)) / bound.max((0, 2))
