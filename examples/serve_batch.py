@@ -137,6 +137,7 @@ class Server:
         def replay():
             graph.replay()
             return out
+        replay.keeps = self, b, pos, embedded        # replays read and write all of it, whoever else still knows it
         return replay
 
 
