@@ -17,6 +17,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2601_11676_amd as H  # noqa: E402
 
 GROUP = 128                                          # neurons per FFN group
+ROWS = 4096                                          # queries that one call of halo_paged_attention takes at most
 
 
 class Config:
@@ -57,6 +58,7 @@ class Server:
         # pages are handed out as sequences grow: here all at once, in scattered order
         self.table = torch.randperm(sequences * per_seq, device="cuda", generator=g).to(torch.int32).view(sequences, per_seq)
         self.lens = torch.zeros(sequences, dtype=torch.int32, device="cuda")
+        self.cached = [0] * sequences                # the same as the host counts it
         self.rope = torch.from_numpy(H.halo_rope_table(longest, c.head_dim)).cuda()
         self.longest = longest
         self.blocks = [Block(c, self.shape, g) for _ in range(c.blocks)]
@@ -103,33 +105,59 @@ class Server:
             H.halo_block_norm(b["h"], b["y"], b["x"], res_scale=0.9, w_pre=after)
         return b["x"]
 
+    def room(self, counts):
+        """Refuses counts[i] new tokens of sequence i where there is no room for them."""
+        if len(counts) != len(self.cached) or min(counts) < 0:
+            raise ValueError(f"new tokens of {len(self.cached)} sequences expected")
+        for i, (have, new) in enumerate(zip(self.cached, counts)):
+            if have + new > self.longest:
+                raise ValueError(f"sequence {i} holds {have} tokens: no room for {new} more, {self.longest} is the longest")
+
     def prompt(self, embedded, counts):
         """New tokens of all sequences at once, counts[i] of sequence i, one after the other in `embedded`: every token attends over what is
-        cached up to itself."""
-        seq = torch.repeat_interleave(torch.arange(len(counts), dtype=torch.int32), torch.tensor(counts)).cuda()
-        at = torch.cat([torch.arange(n, dtype=torch.int32) for n in counts]).cuda()
+        cached up to itself.  Of more than ROWS tokens, a part of them after the other: each finds its sequence's earlier ones in the cache."""
+        self.room(counts)
+        if len(embedded) != sum(counts):
+            raise ValueError(f"{sum(counts)} tokens expected")
+        new = torch.tensor(counts, dtype=torch.int32)
+        seq = torch.repeat_interleave(torch.arange(len(counts), dtype=torch.int32), new).to(self.lens.device)
+        at = torch.cat([torch.arange(n, dtype=torch.int32) for n in counts]).to(self.lens.device)
         pos = (at + self.lens[seq.long()]).to(torch.int32)
-        self.lens += torch.tensor(counts, dtype=torch.int32, device="cuda")
-        return self.step(self.buffers(len(seq)), embedded, pos, seq, self.table[seq.long()].contiguous(), pos + 1, self.longest)
+        parts = []
+        for i in range(0, len(seq), ROWS):
+            e, p, s = embedded[i:i + ROWS], pos[i:i + ROWS], seq[i:i + ROWS]
+            parts.append(self.step(self.buffers(len(s)), e, p, s, self.table[s.long()].contiguous(), p + 1, self.longest))
+        self.lens += new.to(self.lens.device)
+        self.cached = [have + n for have, n in zip(self.cached, counts)]
+        return parts[0] if len(parts) == 1 else torch.cat(parts) if parts else torch.empty_like(embedded)
 
     def decoder(self, embedded, eager=False):
         """One token of each sequence, in `embedded`, per call; captured into a graph once.  max_len bounds every replay's lengths."""
-        b, pos = self.buffers(len(self.lens)), torch.empty_like(self.lens)
+        b, lens = self.buffers(len(self.lens)), torch.empty_like(self.lens)
 
         def one():
-            pos.copy_(self.lens)
+            torch.add(self.lens, 1, out=lens)        # with the new token
+            x = self.step(b, embedded, self.lens, None, self.table, lens, self.longest)
             self.lens.add_(1)
-            return self.step(b, embedded, pos, None, self.table, self.lens, self.longest)
+            return x
+
+        def counted(run):
+            def token():
+                self.room([1] * len(self.cached))
+                x = run()
+                self.cached = [have + 1 for have in self.cached]
+                return x
+            return token
 
         if eager:
-            return one
-        lens = self.lens.clone()
+            return counted(one)
+        before = self.lens.clone()
         side = torch.cuda.Stream()                   # once outside the capture, as a program warms up
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             one()
         torch.cuda.current_stream().wait_stream(side)
-        self.lens.copy_(lens)
+        self.lens.copy_(before)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             out = one()
@@ -137,8 +165,8 @@ class Server:
         def replay():
             graph.replay()
             return out
-        replay.keeps = self, b, pos, embedded        # replays read and write all of it, whoever else still knows it
-        return replay
+        replay.keeps = self, b, lens, embedded       # replays read and write all of it, whoever else still knows it
+        return counted(replay)
 
 
 def main():

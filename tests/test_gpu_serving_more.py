@@ -35,3 +35,26 @@ def test_replays_beside_tensors_made_after_the_capture(dtype, tolerance):
         close(got, want, tolerance)
     for j, t in enumerate(mine):
         assert bool((t == 7 + j // 27).all()), (j, t.dtype, t.numel())
+
+
+@pytest.mark.parametrize("dtype,tolerance", [("f32", 2e-3), ("bf16", 0.15)])
+def test_prompts_of_more_tokens_than_a_call_takes(dtype, tolerance):
+    # at once, in two parts of the server's own making, against calls of fewer tokens; heads and groups all kept, so that no choice between
+    # nearly equal scores tells the two apart
+    from serve_batch import Config, Server
+    c = Config(d=256, heads=8, kv_heads=2, head_dim=32, ffn_groups=6, rank=32, blocks=2, keep_heads=1.0, keep_groups=1.0, dtype=dtype)
+    once, parts = Server(c, 3, 5000), Server(c, 3, 5000)
+    counts = [4500, 1, 700]
+    g = torch.Generator().manual_seed(6)
+    embedded = [torch.randn(n, c.d, generator=g).to(once.shape.torch_dtype).cuda() for n in counts]
+    got = once.prompt(torch.cat(embedded), counts)
+    first = parts.prompt(torch.cat([embedded[0][:2000], embedded[2]]), [2000, 0, 700])
+    second = parts.prompt(torch.cat([embedded[0][2000:], embedded[1]]), [2500, 1, 0])
+    torch.cuda.synchronize()
+    want = torch.cat([first[:2000], second, first[2000:]])
+    assert once.lens.tolist() == parts.lens.tolist() == counts
+    for rows in (slice(0, 4096), slice(4096, None), slice(4499, 4501), slice(-1, None)):
+        close(got[rows], want[rows], tolerance)
+    token_in = torch.randn(3, c.d, generator=g).to(once.shape.torch_dtype).cuda()
+    close(once.decoder(token_in)(), parts.decoder(token_in, True)(), tolerance)
+    torch.cuda.synchronize()
