@@ -423,7 +423,7 @@ int halo_paged_append(const halo_paged_shape *shape, int32_t N, const void *q, i
  *   page_table [T][max_pages], lens [T] int32 on the device
  *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
  *   mask [T][n_heads] uint8: a head whose byte is 0 gives out = 0, and the cache of heads without a surviving query is not read; NULL = all survive.
- * Positions in pages that are no pages count as absent.  A sequence without positions gives out = 0.
+ * Positions in pages that are no pages count as absent.  A sequence without positions gives out = 0; scores that are all -infinity give NaN, as the formula has no value there.
  * How the work is cut depends on the arguments that the host sees (T, max_len, the shape) and, for long ones, on the lengths; results do not depend on timing.
  * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (T outside 0..4096, max_len, stride, alignment, scale not finite, or more than
  * 2^30 tiles of 16 positions in all), HALO_ERR_WORKSPACE, HALO_ERR_HIP.  halo_paged_workspace_bytes: the workspace of up to T sequences; 0 for

@@ -514,19 +514,21 @@ template <typename Core>
 struct Step {
     __amdgpu_buffer_rsrc_t k[Core::kSub], v[Core::kSub];
     int live[Core::kSub];                            // tokens of the 16 that count
-    bool whole;
+    bool whole, any;
 
     __device__ __forceinline__ Step(const AttendArgs &a, Tiles<Core> &tiles, int kv, int len, int i)
     {
         constexpr int kBytes = sizeof(typename Core::Elem);
         if (i - tiles.from >= Tiles<Core>::kHeld) tiles.fetch(i);
         whole = true;
+        any = false;
 #pragma unroll
         for (int p = 0; p < Core::kSub; ++p) {
             const int pos = tiles.position(i) + p * 16;
             const int64_t row = paged_row(a.pool, tiles.page(i, p), kv, pos);
             live[p] = same(row < 0 ? 0 : max(0, min(len - pos, 16)));
             whole = whole && live[p] == 16;
+            any = any || live[p] > 0;
             const uint64_t bytes = (uint64_t)(row < 0 ? 0 : row) * (a.D * kBytes);
             const uint64_t at = (uint64_t)(uint32_t)same((int)(bytes >> 32)) << 32 | (uint32_t)same((int)bytes);
             k[p] = buffer_of(static_cast<const char *>(a.k) + at, live[p] * a.D * kBytes);
@@ -536,7 +538,8 @@ struct Step {
 };
 
 // The part of a step between its products: scores -> probabilities, with the running maximum.  The maximum only moves when a score passes it by 8
-// (a factor of 256, which float sums take with ease), so that most steps rescale nothing.
+// (a factor of 256, which float sums take with ease), so that most steps rescale nothing.  A step with tokens that count lifts it to the lowest float at least,
+// so that one of -infinity says "no positions": a row of scores that are all -infinity has a sum of 0 and gives 0 / 0.
 template <typename Core>
 __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, float scale2, float (&x)[Core::QT][4 * Core::kSub])
 {
@@ -552,7 +555,7 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
         float top = x[t][0];
 #pragma unroll
         for (int e = 1; e < N; ++e) top = fmaxf(top, x[t][e]);
-        top = core.top(top);
+        top = fmaxf(core.top(top), st.any ? -__FLT_MAX__ : -INFINITY);
         const bool passed = top > core.m[t] + 8.0f;
         if (__ballot(passed)) {
             const float to = passed ? top : core.m[t];   // a query's own scores decide: its result does not depend on its neighbours
@@ -681,7 +684,7 @@ struct Joined {
         for (int w = 0; w < waves; ++w) m = fmaxf(m, stats[w * stats_stride + n].x);
         for (int w = 0; w < waves; ++w) {
             const float2 ml = stats[w * stats_stride + n];
-            const bool none = ml.y == 0.0f;          // no positions: nothing was stored
+            const bool none = ml.x == -INFINITY;     // no positions: nothing was stored
             const float by = none ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
             const float4 v = *reinterpret_cast<const float4 *>(part + w * part_stride + i * 4);
             l += ml.y * by;
@@ -694,8 +697,7 @@ struct Joined {
     template <typename T>
     __device__ __forceinline__ void store(T *to, bool kept) const
     {
-        // a sum of 0 is a row without positions; NaN has to come through
-        const bool none = l == 0.0f || !kept;
+        const bool none = m == -INFINITY || !kept;
         const float by = 1.0f / l;
         const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
         store_piece(to, v);
@@ -910,8 +912,7 @@ __global__ __launch_bounds__(kTeam * 64, Core::kWaves) void attend_stream(Attend
 #pragma unroll
                 for (int q = 0; q < Core::QT; ++q) {
                     const int i = q * kCols + core.col();
-                    // a sum of 0 is a row without positions; NaN has to come through
-                    by[q] = i >= unit.nq || !head_alive(a, t, unit.head + i) || l[q] == 0.0f ? 0.0f : 1.0f / l[q];
+                    by[q] = i >= unit.nq || !head_alive(a, t, unit.head + i) || core.m[q] == -INFINITY ? 0.0f : 1.0f / l[q];
                 }
                 store_rows(core, static_cast<typename Core::Elem *>(a.out) + ((int64_t)t * a.n_heads + unit.head) * core.D, unit.nq, by);
             } else if (at < end) {                   // the share goes on: a partial result of its own
@@ -1008,7 +1009,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a)
                 for (int k = 1; k < kShares; ++k) take_in(m, l, o, s_ml[k * kQuads + tid], s_o[k * kQuads + tid]);
         }
         if (share == 0 && i < quads) {
-            const bool none = l == 0.0f || !kept;
+            const bool none = m == -INFINITY || !kept;
             const float by = 1.0f / l;
             const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
             store_piece(out + i * 4, v);

@@ -87,3 +87,44 @@ def test_probabilities_are_as_fine_as_floats(Hq, Hk, D, length, max_len):
     bound = r * F * (2 * (np.abs(s.numpy()).repeat(Hq // Hk)[None, :, None] + 1) + 12) / (2 + r) + 2.0 ** -8 * np.abs(want)
     assert np.all(np.abs(want) > 1.5 * bound)                         # two parts alone would give 0
     assert np.all(np.abs(got - want) <= bound), np.abs(got - want).max((0, 2)) / bound.max((0, 2))
+
+
+# ---------------------------------------------------------------- scores of -infinity
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hk,D,length,max_len", [
+    (4, 2, 64, 40, 40), (4, 2, 64, 200, 200), (6, 2, 128, 900, 900), (2, 2, 256, 700, 700), (32, 2, 96, 300, 300), (2, 2, 64, 6000, 6000),
+    (32, 2, 128, 3000, 3000), (4, 2, 256, 2500, 2500), (80, 2, 128, 400, 200000), (80, 2, 64, 9000, 200000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_of_minus_infinity(dtype, Hq, Hk, D, length, max_len):
+    # keys of -infinity in the dimension that a query asks for: such a token counts for nothing beside others (weight 0), and where all are like that the
+    # formula has no value (0 / 0).  Sequences, of the first cache head: all; all but the last five; all but the first seven; all but some in the middle; all, some of the
+    # pages being none; no page at all; none.  The other cache head has none of them but in the last sequence, which has all.
+    lens = [length] * 6 + [length - 3]
+    shape, table, lens, pools = paged(dtype, Hq, Hk, D, 16, lens, max_len, seed=1)
+    g = torch.Generator().manual_seed(2)
+    values = []
+    for t, n in enumerate(lens.tolist()):
+        k, v = torch.zeros(n, Hk, D), torch.randint(-4, 5, (n, Hk, D), generator=g).float()
+        k[:, :, 0] = -torch.randint(0, 6, (n, Hk), generator=g).float()
+        none = torch.ones(n, dtype=torch.bool)
+        if 1 <= t <= 3:
+            none[[slice(n - 5, n), slice(0, 7), slice(n // 2, n // 2 + 20)][t - 1]] = False
+        k[none & (t < 6), 0, 0] = -torch.inf
+        if t == 6:
+            k[:, 1, 0] = -torch.inf
+        put(pools[0], table, t, k)
+        put(pools[1], table, t, v)
+    table[4, 1::2] = -1
+    table[5] = shape.n_pages
+    q = torch.zeros(7, Hq, D, dtype=DT[dtype])
+    q[:, :, 0] = 1.0
+    got, want = attend(shape, table, lens, pools, q, max_len), wanted(table, lens, pools, q)
+    half = Hq // 2
+    empty = np.zeros((7, Hq), dtype=bool)
+    empty[[0, 4], :half] = empty[6, half:] = True
+    assert np.array_equal(np.isnan(want).all(-1), empty) and np.array_equal(np.isnan(want).any(-1), empty)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.all(got[5] == 0)
+    # probabilities off by 2 (|s| + 1) F, at most 14 F, sums in any order by F a term, in the numerator and in the sum; values up to 4
+    bound = 2.0 ** -8 * (dtype == "bf16") * np.abs(want) + 4 * 2 * (14 + length) * F
+    assert np.all((np.abs(got - want) <= bound) | empty[..., None])
