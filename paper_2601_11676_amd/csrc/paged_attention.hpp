@@ -85,7 +85,15 @@ struct KeyPlace {
     __device__ __forceinline__ uint32_t get(int s) const { return out ^ (s << 6); }
 };
 
-// A step's keys: loaded rows in, the lane's pieces out.  A wave's LDS accesses keep their order: nothing to wait for in between.
+// Between LDS accesses of lanes that use each other's: the hardware keeps a wave's in order, so that there is nothing to wait for, but the compiler, which
+// sees one lane, has to be told.  No instruction comes of it.
+__device__ __forceinline__ void wave_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A step's keys: loaded rows in, the lane's pieces out.
 template <typename Core>
 __device__ __forceinline__ void turn_keys(Core &core)
 {
@@ -93,6 +101,7 @@ __device__ __forceinline__ void turn_keys(Core &core)
     for (int i = 0; i < Core::kSub; ++i)
 #pragma unroll
         for (int s = 0; s < Core::KS; ++s) *reinterpret_cast<u32x4 *>(core.lds + i * 16 * core.keys.kBytes + core.keys.put(s)) = __builtin_bit_cast(u32x4, core.kf[i][s]);
+    wave_in_order();
 #pragma unroll
     for (int i = 0; i < Core::kSub; ++i)
 #pragma unroll
@@ -100,6 +109,7 @@ __device__ __forceinline__ void turn_keys(Core &core)
             const u32x4 v = *reinterpret_cast<const u32x4 *>(core.lds + i * 16 * core.keys.kBytes + core.keys.get(s));
             core.kf[i][s] = __builtin_bit_cast(std::remove_reference_t<decltype(core.kf[i][s])>, v);
         }
+    wave_in_order();                                 // before the next step's rows, or the results, take the place
 }
 
 // The running softmax of one unit over bf16 rows, kSub times 16 tokens a step.  DP = head dimension, or the next of 64, 128, 256 above it (EXACT false).
