@@ -366,7 +366,7 @@ int halo_mha_forward_ahead(const halo_mha_shape *shape, const void *x, const voi
 /*
  * Serving a batch of sequences over a paged cache: appending tokens, attending over the pages, and the norms around a block.  With the
  * caller's projections these make an attention block for T sequences, next to an FFN that takes T tokens; surviving heads are those of a mask
- * from halo_build_group_mask with G = n_heads, as in the attention block above.
+ * from halo_build_group_mask with G = n_heads, as in the attention block above.  Calls without tokens (N or T 0) do nothing, and their pointers may be NULL.
  *
  * The cache is two pools of pages, k_pages and v_pages, each [n_pages][n_kv_heads][page_size][head_dim] (dtype): one head's tokens of a page
  * are consecutive rows.  page_table [n_seq][max_pages] int32 lists each sequence's pages in order: position p lies in page

@@ -161,13 +161,13 @@ extern "C" int halo_block_norm(const void *h, const void *y, const void *w_post,
                                int32_t gate_per_token, float res_scale, float eps, void *stream)
 {
     using namespace halo;
-    if (!h || !y || !h_out || !x) return HALO_ERR_NULL;
     if (dtype != HALO_F32 && dtype != HALO_BF16) return HALO_ERR_DTYPE;
     if (h_dtype != HALO_F32 && h_dtype != dtype) return HALO_ERR_DTYPE;
     if (T < 0 || d < 8 || d % 8 || d > 32768 || !(eps >= 0.0f) || !std::isfinite(res_scale)) return HALO_ERR_ARG;
+    if (T == 0) return HALO_OK;
+    if (!h || !y || !h_out || !x) return HALO_ERR_NULL;
     for (const void *p : {h, y, w_post, gate, w_pre, (const void *)h_out, (const void *)x})
         if (reinterpret_cast<uintptr_t>(p) & 15u) return HALO_ERR_ARG;
-    if (T == 0) return HALO_OK;
     const NormArgs a{h, y, w_post, gate, w_pre, h_out, x, T, d, post_norm != 0, gate_per_token != 0, res_scale, eps};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (dtype == HALO_F32) return launch_norm<float, float>(a, s);

@@ -159,19 +159,20 @@ extern "C" int halo_paged_append(const halo_paged_shape *shape, int32_t N, const
 {
     using namespace halo;
     if (const int rc = check_paged_shape(shape)) return rc;
+    if (N < 0) return HALO_ERR_ARG;
+    if (N == 0) return HALO_OK;
     if (!k || !v || !pos || !page_table || !k_pages || !v_pages || !q != !q_out) return HALO_ERR_NULL;
     const halo_paged_shape &s = *shape;
     const int size = s.dtype == HALO_F32 ? 4 : 2;
     auto odd = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; };
     auto bad_stride = [&](int64_t stride, int heads) { return stride < (int64_t)heads * s.head_dim || stride * size % 16; };
-    if (N < 0 || n_seq < 1 || (q && (q == q_out || bad_stride(q_stride, s.n_heads))) || bad_stride(k_stride, s.n_kv_heads) ||
+    if (n_seq < 1 || (q && (q == q_out || bad_stride(q_stride, s.n_heads))) || bad_stride(k_stride, s.n_kv_heads) ||
         bad_stride(v_stride, s.n_kv_heads))
         return HALO_ERR_ARG;
     if (odd(q) || odd(k) || odd(v) || odd(q_out) || odd(k_pages) || odd(v_pages) || odd(rope) ||
         ((reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(page_table)) & 3u))
         return HALO_ERR_ARG;
     if (rope && (rope_len < 1 || rotary_dim < 16 || rotary_dim % 16 || rotary_dim > s.head_dim)) return HALO_ERR_ARG;
-    if (N == 0) return HALO_OK;
 
     AppendArgs a{};
     a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages;

@@ -81,17 +81,18 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
 {
     using namespace halo;
     if (const int rc = check_paged_shape(shape)) return rc;
+    if (T < 0 || T > kMaxSeqs) return HALO_ERR_ARG;
+    if (T == 0) return HALO_OK;
     if (!q || !k_pages || !v_pages || !page_table || !lens || !out) return HALO_ERR_NULL;
     const halo_paged_shape &s = *shape;
     const int size = s.dtype == HALO_F32 ? 4 : 2;
     auto odd = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; };
-    if (T < 0 || T > kMaxSeqs || max_len < 1 || max_len > s.max_pages * s.page_size || !std::isfinite(scale)) return HALO_ERR_ARG;
+    if (max_len < 1 || max_len > s.max_pages * s.page_size || !std::isfinite(scale)) return HALO_ERR_ARG;
     if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q) || odd(k_pages) || odd(v_pages) || odd(out) ||
         odd(workspace) || (reinterpret_cast<uintptr_t>(page_table) & 3u) || (reinterpret_cast<uintptr_t>(lens) & 3u))
         return HALO_ERR_ARG;
     const PagedWorkspace ws(s, T);
     if (!workspace || ws_bytes < ws.bytes) return HALO_ERR_WORKSPACE;
-    if (T == 0) return HALO_OK;
 
     AttendArgs a{};
     a.q = q; a.k = k_pages; a.v = v_pages; a.table = page_table; a.lens = lens; a.mask = mask; a.out = out;
