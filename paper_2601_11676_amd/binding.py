@@ -461,6 +461,8 @@ def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pa
     pr, rows, half = None, 0, 0
     if rope is not None:
         rows, _, half = rope.shape
+        if not rows or not half:                     # without an address it would mean no rotation
+            raise ValueError("a table of angles has rows and columns")
         pr = _dense(rope, torch.float32, rows * 2 * half)
     rc = load_library().halo_paged_append(
         shape.c, N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N),

@@ -53,3 +53,15 @@ def test_tensors_of_no_tokens(binding):
     H.halo_block_norm(OnDevice(0, 64, dtype=torch.float32), OnDevice(0, 64), OnDevice(0, 64), post_norm=True, w_post=OnDevice(64), w_pre=OnDevice(64))
     with pytest.raises(H.HaloError):                 # the shape still is
         H.halo_block_norm(OnDevice(0, 60), OnDevice(0, 60), OnDevice(0, 60))
+
+
+def test_a_table_of_no_angles_is_refused(binding):
+    # its address is 0, which to the library means no rotation
+    s, kp, vp = binding
+    k, pos, table = OnDevice(1, 2, 64), OnDevice(1, dtype=torch.int32), OnDevice(1, 4, dtype=torch.int32)
+    rope = OnDevice(0, 2, 32, dtype=torch.float32)
+    rope.data_ptr = lambda: 0                        # as of a device tensor without elements
+    for empty in (rope, OnDevice(4, 2, 0, dtype=torch.float32)):
+        with pytest.raises(ValueError, match="angles"):
+            H.prepared(H.halo_paged_append, s, None, k, k, pos, table, kp, vp, rope=empty)
+    H.prepared(H.halo_paged_append, s, None, k, k, pos, table, kp, vp, rope=OnDevice(1, 2, 32, dtype=torch.float32))
