@@ -5,6 +5,7 @@
 // between its waves (3 to 4 us).
 #include "../../include/halo.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "kernels.hpp"
@@ -15,7 +16,7 @@ namespace {
 struct NormArgs {
     const void *h, *y, *w_post, *gate, *w_pre;
     void *h_out, *x;
-    int T, d, post, gate_per_token;
+    int T, d, post, gate_per_token, first;           // first: row of the launch's first workgroup
     float res_scale, eps;
 };
 
@@ -55,11 +56,11 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void block_norm_kernel(NormArgs 
 {
     __shared__ float s_sum[2][16];
     const int threads = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
-    const int row = WAVE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int64_t row = a.first + (WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x);
     if (WAVE && row >= a.T) return;
-    const HT *h = static_cast<const HT *>(a.h) + (int64_t)row * a.d;
-    const T *y = static_cast<const T *>(a.y) + (int64_t)row * a.d;
-    const T *gate = static_cast<const T *>(a.gate) + (a.gate_per_token ? (int64_t)row * a.d : 0);
+    const HT *h = static_cast<const HT *>(a.h) + row * a.d;
+    const T *y = static_cast<const T *>(a.y) + row * a.d;
+    const T *gate = static_cast<const T *>(a.gate) + (a.gate_per_token ? row * a.d : 0);
     const T *w_post = static_cast<const T *>(a.w_post), *w_pre = static_cast<const T *>(a.w_pre);
 
     // rows of more than 16384 would need more registers than 1024 threads have: their weights are loaded where they are used
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void block_norm_kernel(NormArgs 
             sq = __builtin_fmaf(z[c][i], z[c][i], sq);
         }
         const int e = (c * threads + tid) * 8;
-        if (e < a.d) store8_pass(static_cast<HT *>(a.h_out) + (int64_t)row * a.d + e, z[c]);
+        if (e < a.d) store8_pass(static_cast<HT *>(a.h_out) + row * a.d + e, z[c]);
     }
     by = 1.0f / sqrtf(row_sum<WAVE>(sq, s_sum[1]) / (float)a.d + a.eps);
 #pragma unroll
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void block_norm_kernel(NormArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[c][i] *= a.w_pre ? by * w[i] : by;
         const int e = (c * threads + tid) * 8;
-        if (e < a.d) store8(static_cast<T *>(a.x) + (int64_t)row * a.d + e, z[c]);
+        if (e < a.d) store8(static_cast<T *>(a.x) + row * a.d + e, z[c]);
     }
 }
 
@@ -137,13 +138,22 @@ template <typename T, typename HT>
 int launch_norm(const NormArgs &a, hipStream_t s)
 {
     const int pieces = a.d / 8;
+    // one launch, of rows whose workgroups number less than 2^32 threads; of more rows one after the other
+    auto each_run = [&](int rows_a_group, int threads, auto launch) {
+        const int64_t run = (int64_t)(0xffffffffu / threads) * rows_a_group;
+        for (int64_t first = 0; first < a.T; first += run) {
+            NormArgs part = a;
+            part.first = (int)first;
+            launch(dim3((unsigned)((std::min(run, a.T - first) + rows_a_group - 1) / rows_a_group)), part);
+        }
+    };
     auto rows_of_waves = [&](auto c) {
-        block_norm_kernel<T, HT, decltype(c)::value, true><<<dim3((a.T + 3) / 4), dim3(256), 0, s>>>(a);
+        each_run(4, 256, [&](dim3 grid, const NormArgs &p) { block_norm_kernel<T, HT, decltype(c)::value, true><<<grid, dim3(256), 0, s>>>(p); });
     };
     auto row_of_workgroup = [&](auto c) {
         constexpr int C = decltype(c)::value;
         const int threads = ((pieces + C - 1) / C + 63) / 64 * 64;
-        block_norm_kernel<T, HT, C, false><<<dim3(a.T), dim3(threads), 0, s>>>(a);
+        each_run(1, threads, [&](dim3 grid, const NormArgs &p) { block_norm_kernel<T, HT, C, false><<<grid, dim3(threads), 0, s>>>(p); });
     };
     // two pieces a thread from 513 on: 4099 rows of 5120 44.3 us with one, 41.6 with two
     if (pieces <= 64) rows_of_waves(std::integral_constant<int, 1>{});
@@ -168,7 +178,7 @@ extern "C" int halo_block_norm(const void *h, const void *y, const void *w_post,
     if (!h || !y || !h_out || !x) return HALO_ERR_NULL;
     for (const void *p : {h, y, w_post, gate, w_pre, (const void *)h_out, (const void *)x})
         if (reinterpret_cast<uintptr_t>(p) & 15u) return HALO_ERR_ARG;
-    const NormArgs a{h, y, w_post, gate, w_pre, h_out, x, T, d, post_norm != 0, gate_per_token != 0, res_scale, eps};
+    const NormArgs a{h, y, w_post, gate, w_pre, h_out, x, T, d, post_norm != 0, gate_per_token != 0, 0, res_scale, eps};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (dtype == HALO_F32) return launch_norm<float, float>(a, s);
     return h_dtype == HALO_F32 ? launch_norm<bf16_t, float>(a, s) : launch_norm<bf16_t, bf16_t>(a, s);

@@ -8,6 +8,7 @@
 // reaches 4.8), 112 MB of float 21.9 -> 18.3; runs of 80 bytes (heads of 80, bf16) 12.3 -> 15.5, so these do without it.
 #include "../../include/halo.h"
 
+#include <algorithm>
 #include <cmath>
 
 #include "kernels.hpp"
@@ -29,6 +30,7 @@ struct AppendArgs {
     int64_t q_stride, k_stride, v_stride;
     PagePool pool;
     int n_heads, D, max_pages, n_seq, max_pos, rotary, pairs;
+    int first;                                       // token of the launch's first workgroup
 };
 
 // 16 bytes of a head
@@ -60,7 +62,7 @@ template <typename T, bool PASS>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a)
 {
     constexpr int E = Piece<T>::kElems;
-    const int token = blockIdx.x, places = a.D / (2 * E), heads_at_once = kAppendThreads / places;
+    const int token = a.first + blockIdx.x, places = a.D / (2 * E), heads_at_once = kAppendThreads / places;
     const int place = threadIdx.x % places, row = threadIdx.x / places + blockIdx.y * heads_at_once;
     const int k_from = a.q ? a.n_heads : 0, v_from = k_from + a.pool.n_kv, rows = v_from + a.pool.n_kv;
     if ((int)threadIdx.x >= heads_at_once * places || row >= rows) return;
@@ -188,14 +190,19 @@ extern "C" int halo_paged_append(const halo_paged_shape *shape, int32_t N, const
     const int faced = rope && !rope_pairs ? rotary_dim : 0;
     const bool runs = (faced / 2 * size | (s.head_dim - faced) / 2 * size | s.head_dim / 2 * size) % 64 == 0;
     const bool pass = runs && (int64_t)N * rows * s.head_dim * size >= (4 << 20);
-    const dim3 grid(N, (rows + at_once - 1) / at_once), threads(kAppendThreads);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (s.dtype == HALO_F32) {
-        if (pass) append_kernel<float, true><<<grid, threads, 0, st>>>(a);
-        else append_kernel<float, false><<<grid, threads, 0, st>>>(a);
-    } else {
-        if (pass) append_kernel<bf16_t, true><<<grid, threads, 0, st>>>(a);
-        else append_kernel<bf16_t, false><<<grid, threads, 0, st>>>(a);
+    // one launch, of tokens whose workgroups number less than 2^32 threads; of more tokens one after the other
+    constexpr int64_t kRun = 0xffffffffu / kAppendThreads;
+    for (int64_t first = 0; first < N; first += kRun) {
+        a.first = (int)first;
+        const dim3 grid((unsigned)std::min(kRun, N - first), (rows + at_once - 1) / at_once), threads(kAppendThreads);
+        if (s.dtype == HALO_F32) {
+            if (pass) append_kernel<float, true><<<grid, threads, 0, st>>>(a);
+            else append_kernel<float, false><<<grid, threads, 0, st>>>(a);
+        } else {
+            if (pass) append_kernel<bf16_t, true><<<grid, threads, 0, st>>>(a);
+            else append_kernel<bf16_t, false><<<grid, threads, 0, st>>>(a);
+        }
     }
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
