@@ -128,3 +128,53 @@ def test_scores_of_minus_infinity(dtype, Hq, Hk, D, length, max_len):
     # probabilities off by 2 (|s| + 1) F, at most 14 F, sums in any order by F a term, in the numerator and in the sum; values up to 4
     bound = 2.0 ** -8 * (dtype == "bf16") * np.abs(want) + 4 * 2 * (14 + length) * F
     assert np.all((np.abs(got - want) <= bound) | empty[..., None])
+
+
+# ---------------------------------------------------------------- every position once
+def marked(n, Hk, D, seed):
+    """Values of n tokens: dimension 0 is 1; of the others each sums to exactly 0 over the tokens, +1 and -1 in random order (with an odd n one of them 0)."""
+    g = torch.Generator().manual_seed(seed)
+    signs = torch.cat([torch.ones(n // 2), -torch.ones(n // 2), torch.zeros(n % 2)])
+    v = signs[torch.rand(Hk * (D - 1), n, generator=g).argsort(1)].view(Hk, D - 1, n).permute(2, 0, 1)
+    return torch.cat([torch.ones(n, Hk, 1), v], dim=2)
+
+
+LONG = [("bf16", 8, 8, 128, 16, [2000, 1, 0, 1025, 3001]), ("bf16", 64, 8, 128, 64, [5003]), ("f32", 4, 2, 64, 32, [3000, 40]), ("bf16", 20, 1, 256, 256, [1100, 64]),
+        ("f32", 2, 1, 240, 16, [1100, 900]), ("bf16", 1, 1, 128, 4096, [9000]), ("f32", 6, 6, 112, 16, [1030, 2, 1500]), ("f32", 1, 1, 16, 16, [6000]),
+        ("bf16", 16, 2, 64, 16, [50 + 37 * i for i in range(70)]), ("bf16", 34, 2, 80, 64, [9000, 4001]), ("f32", 10, 2, 128, 16, [2000, 45, 700]),
+        ("f32", 4, 1, 32, 16, [7000, 2]), ("f32", 20, 1, 16, 16, [40000, 30000, 5]), ("bf16", 8, 2, 48, 16, [33333, 16, 20001]),
+        ("bf16", 40, 2, 96, 32, [60000]), ("f32", 40, 2, 128, 16, [30011, 333]), ("bf16", 4, 4, 256, 16, [7777, 700, 2]), ("f32", 3, 1, 256, 16, [5555, 16]),
+        ("bf16", 32, 32, 128, 16, [301]), ("bf16", 8, 8, 64, 32, [3 * i for i in range(80)]), ("f32", 16, 16, 128, 16, [500 + i % 100 for i in range(64)])]
+
+
+@pytest.mark.parametrize("args", LONG, ids=lambda a: "-".join(map(str, a[:5])) + f"-{max(a[5])}x{len(a[5])}")
+def test_marks_show_what_is_lost_or_doubled(args):
+    # what the next test could not see does not happen: any token alone, and any run of 16, 32, 64 or 256 that a share may end in, has a sum other than 0
+    # in some dimension
+    _, _, Hk, D, _, lens = args
+    for t, n in enumerate(lens):
+        v = marked(n, Hk, D, t)[:, :, 1:]
+        assert bool((v.sum(0) == 0).all())
+        for run in (1, 16, 32, 64, 256):
+            if run < n:
+                sums = torch.stack([v[i:i + run].sum(0) for i in range(0, n, run)])
+                assert bool((sums != 0).any(-1).all()), (n, run)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bound", ["exact", "larger"])
+@pytest.mark.parametrize("args", LONG, ids=lambda a: "-".join(map(str, a[:5])) + f"-{max(a[5])}x{len(a[5])}")
+def test_every_position_counts_once(args, bound):
+    # Scores of 0: every probability is 1, the sums are of whole numbers below 2^24 and exact in any order.  The results are 0, but 1 in the first dimension: the
+    # number of positions times its reciprocal, off by two roundings and the result's.
+    dtype, Hq, Hk, D, page, lens = args
+    max_len = max(lens) if bound == "exact" else 3 * max(lens) + 2100
+    shape, table, lens, pools = paged(dtype, Hq, Hk, D, page, lens, max_len, seed=3)
+    g = torch.Generator().manual_seed(4)
+    for t, n in enumerate(lens.tolist()):
+        put(pools[0], table, t, torch.randn(n, Hk, D, generator=g))
+        put(pools[1], table, t, marked(n, Hk, D, t))
+    got = attend(shape, table, lens, pools, torch.zeros(len(lens), Hq, D, dtype=DT[dtype]), max_len)
+    some = lens.numpy() > 0
+    assert np.all(got[:, :, 1:] == 0) and np.all(got[~some] == 0)
+    assert np.all(np.abs(got[some][:, :, 0] - 1) <= 3 * F + 2.0 ** -8 * (dtype == "bf16"))
