@@ -1042,7 +1042,7 @@ int launch_stream(const AttendArgs &a, hipStream_t s)
 {
     typedef typename Core::Elem Elem;
     const int pairs = a.T * a.n_units, tiles = (a.max_len + Core::kTile - 1) / Core::kTile;
-    const size_t lds = (2 * (size_t)a.T + 1) * sizeof(int);          // at most 32 KiB
+    const size_t lds = (2 * (size_t)a.T + 1) * sizeof(int);          // at most 32 KiB and 4 bytes, beside up to 66 KiB that the kernel has of its own (of 160)
     constexpr int grid = kUnits * Core::kWaves;                      // what is resident at once: with rows of 256 half as much
     const int64_t wanted = ((int64_t)pairs * tiles + kTeam * Core::kLeast - 1) / (kTeam * Core::kLeast);
     attend_stream<Core><<<dim3(wanted < grid ? (int)wanted : grid), dim3(kTeam * 64), lds, s>>>(a);

@@ -178,3 +178,18 @@ def test_every_position_counts_once(args, bound):
     some = lens.numpy() > 0
     assert np.all(got[:, :, 1:] == 0) and np.all(got[~some] == 0)
     assert np.all(np.abs(got[some][:, :, 0] - 1) <= 3 * F + 2.0 ** -8 * (dtype == "bf16"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,Hq,Hk,D", [("bf16", 1, 1, 256), ("f32", 8, 1, 240), ("bf16", 32, 1, 128), ("f32", 32, 1, 128), ("f32", 4, 2, 64), ("bf16", 2, 1, 64)])
+def test_as_many_sequences_as_there_can_be(dtype, Hq, Hk, D):
+    # 4096 short caches under a bound that takes the kernel of even shares: it has the line of all tiles in LDS beside its own part, at its longest here
+    lens, max_len = [(i * 7) % 40 for i in range(4095)] + [3000], 20000
+    shape, table, lens, pools = paged(dtype, Hq, Hk, D, 16, lens, max_len, seed=5)
+    for t, n in enumerate(lens.tolist()):
+        put(pools[0], table, t, torch.zeros(n, Hk, D))
+        put(pools[1], table, t, marked(n, Hk, D, t % 40))
+    got = attend(shape, table, lens, pools, torch.zeros(len(lens), Hq, D, dtype=DT[dtype]), max_len)
+    some = lens.numpy() > 0
+    assert np.all(got[:, :, 1:] == 0) and np.all(got[~some] == 0)
+    assert np.all(np.abs(got[some][:, :, 0] - 1) <= 3 * F + 2.0 ** -8 * (dtype == "bf16"))
