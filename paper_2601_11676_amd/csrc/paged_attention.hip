@@ -104,9 +104,10 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
     a.T = T; a.n_heads = s.n_heads; a.group = s.n_heads / s.n_kv_heads;
     a.bytes = most_bytes(s, T, max_len);
-    // More than 16 queries a cache head: 32 at once read the cache once, 16 at a time have more workgroups.  us, 32 / 16: 16 sequences of up to 8000, 8 cache heads
-    // with 20 queries (360 MB) 78 / 127; 30 of up to 5000, 2 with 20, heads of 96 (69 MB) 30.5 / 36.4; 8 of up to 700, 2 with 20 (4 MB) 15.7 / 11.6.
-    // Float, 8 cache heads with 20 queries: 24 of up to 5000 135 / 228; 4 of up to 4000 (131 MB) 32.9 / 41.9; 4 of up to 1000 (32 MB) 21.5 / 21.0; 1 of 1000 19.7 / 15.0.
+    // More than 16 queries a cache head: 32 at once read the cache once, 16 at a time have more workgroups.  us, 32 / 16, lengths from half of the longest on: 16 sequences of up to
+    // 8000, 8 cache heads with 20 queries (524 MB at the longest) 77 / 134; 30 of up to 5000, 2 with 20, heads of 96 (115 MB) 27.5 / 36.7; 8 of up to 700, 2 with 20 (6 MB)
+    // 12.3 / 8.3.  Float, 8 cache heads with 20 queries: 24 of up to 5000 150 / 243; 4 of up to 4000 (131 MB) 31.8 / 40.6; 4 of up to 1000 (33 MB) 20.6 / 20.2; 1 of 1000
+    // 18.8 / 14.4.
     a.rows = rows_of_unit(s, a.bytes > (64 << 20) ? most_rows(s) : kCols);
     a.n_qt = (a.group + a.rows - 1) / a.rows;
     a.n_units = s.n_kv_heads * a.n_qt;

@@ -61,13 +61,13 @@ __device__ __forceinline__ V row_load(__amdgpu_buffer_rsrc_t rows, uint32_t at)
 }
 
 // Which of the cache's rows carry the non-temporal hint: none, the values, both.  What passes through once should not push out what stays; with
-// caches that fit the dies' L2 the hint costs.  us, by the bytes of the call, none / values / both: 18 MB 9.4 / 11.3 / 11.6; 98 MB 19.4 / 18.5 / 19.3;
-// 134 MB 36.4 / 31.3 / 32.3; 738 MB 140 / 127 / 123; 1.7 GB 316 / 286 / 281.
+// caches that fit the dies' L2 the hint costs.  us, by the bytes of the call at its longest length, none / values / both: 33 MB 9.6 / 11.9 / 12.0; 131 MB 19.0 / 18.7 /
+// 19.1; 262 MB 38.7 / 33.9 / 34.5; 524 MB 72.4 / 66.1 / 64.6; 885 MB 79.4 / 72.4 / 70.6; 3.2 GB 285 / 283 / 278.
 enum { kKeepAll = 0, kPassValues = 1, kPassBoth = 2 };
 
 // Keys on their way from whole rows, as they are loaded, to the lanes that multiply them: 16 rows of DP elements in LDS, piece p of row r at place
 // p ^ r (within 16), so that neither side meets a bank twice.  kRows rows a load; the same number of loads as of pieces a lane gets.  (With each lane
-// loading its pieces itself, 8 sequences of up to 1000 took 12.8 us, now 9.0.)
+// loading its pieces itself, 8 sequences of up to 1000 took 12.8 us, then 9.0.)
 template <typename Elem, int DP>
 struct KeyPlace {
     static constexpr int kBytes = DP * sizeof(Elem), kPieces = kBytes / 16, kRows = 64 / kPieces;
@@ -269,7 +269,8 @@ template <int DP, bool EXACT, int HINT> using CoreBf16One = CoreBf16<DP, EXACT, 
 template <int DP, bool EXACT, int HINT> using CoreBf16Two = CoreBf16<DP, EXACT, HINT, 2>;
 
 // The same over float rows: every operand of the matrix instruction is one float a lane.  With 32 queries and rows of 128 one wave a SIMD, which has
-// 350 registers; two with 256 each take 153 us where one takes 135 (24 sequences of up to 5000, 8 cache heads of 20 queries).
+// 350 registers; two with 256 each take 163 us where one takes 150 (24 sequences of 2500 to 5000, 8 cache heads of 20 queries; floor 106).  A workgroup that
+// takes a pair has eight waves here too, which spill 9 registers with heads of 80 to 112.
 template <int DP, bool EXACT, int HINT, int TILES>
 struct CoreF32 {
     typedef float Elem;
@@ -1070,10 +1071,10 @@ int launch_pairs(const AttendArgs &a, hipStream_t s)
 // One launch, a workgroup a pair, or even shares and a second launch: the latter costs some 5 us more, the former is as slow as its longest pair on one compute unit.
 // One launch up to kSteps steps of a wave (8; 4 and 6 where a step computes longer) at the longest length; from 512 pairs on, two for every unit, up to 8, or 16
 // with rows of 256, of which a unit has half as many waves.  us, one launch / two (lengths from half of the longest to the longest):
-// bf16 heads of 128, 8 cache heads, 1 sequence of 1024 8.6 / 12.0, 2048 (8 steps) 12.5 / 12.2, 4096 23 / 13; 16 sequences 2048 22.3 / 26.7, 4096 44.4 / 42.9; 64
-// sequences 2048 66.5 / 73.4, 4096 134 / 134, and with lengths from 0 on 127 to 131 / 125.  Heads of 64, 1 sequence of 2048 (4 steps) 12.8 / 12.5; 64 of 4000 (8) 85 / 93.
-// Heads of 256, 8 sequences of 1024 (8 steps) 17.2 / 22.1, 64 of 2048 (16) 129 / 149.  Float heads of 64, four queries a cache head, 1 sequence of 1024
-// 10.5 / 11.7, 2048 (8 steps) 16.1 / 11.8; 8 sequences 2048 15.9 / 18.7; 64 sequences 2048 65.5 / 72.2.
+// bf16 heads of 128, 8 cache heads, 1 sequence of 1024 8.7 / 10.6, 2048 (8 steps) 13.5 / 11.1, 4096 23.4 / 11.7; 16 sequences 2048 21.4 / 25.1, 4096 44.1 / 41.3; 64
+// sequences 2048 66.0 / 71.6, 4096 134 / 135, and with lengths from 0 on 102 / 94.  Heads of 64, 1 sequence of 2048 (4 steps) 10.9 / 11.4; 64 of 4000 (8) 69 / 71.
+// Heads of 256, 8 sequences of 1024 (8 steps) 16.2 / 21.1, 64 of 2048 (16) 127 / 135.  Float heads of 64, four queries a cache head, 1 sequence of 1024
+// 9.2 / 10.9, 2048 (8 steps) 14.7 / 11.2; 8 sequences 2048 15.2 / 17.8; 64 sequences 2048 66.7 / 70.1.
 template <template <int, bool, int> class Core, int DP, bool EXACT>
 int launch_cut(const AttendArgs &a, hipStream_t s)
 {
@@ -1082,9 +1083,9 @@ int launch_cut(const AttendArgs &a, hipStream_t s)
     const int steps = !many ? C::kSteps : DP > 128 ? 16 : 8;
     const bool one_launch = a.max_len <= steps * C::kItemWaves * C::kTile;
     // Fewer waves a workgroup where more would have no tile, and where workgroups are many anyway: all of their waves wait for the slowest.
-    // us, heads of 128, 8 cache heads, by waves 8 / 4 / 2: 1 sequence of up to 64 (2 tiles) 3.9 / 3.7 / 3.6, of 128 4.1 / 4.1 / 4.6; 128 sequences of 16 10.2 / 7.0 /
-    // 4.5, of 256 (8 tiles) 21.8 / 18.4 / 18.1; 192 of 300 (10) 34.7 / 29.7 / 31.4, of 600 (19) 58.2 / 58.6 / 61.8; 32 of 128, 256 pairs, 5.1 / 5.0 / 5.2.  With 20
-    // queries a cache head, 8 / 2: 200 sequences of up to 250 44.7 / 31.9, 500 of up to 60 in float 123 / 72.5; 100 of up to 500, 8 / 4, 35.7 / 36.0.
+    // us, heads of 128, 8 cache heads, by waves 8 / 4 / 2: 1 sequence of up to 64 (2 tiles) 4.1 / 4.0 / 4.0, of 128 4.3 / 4.2 / 4.7; 128 sequences of 16 12.3 / 7.0 /
+    // 4.6, of 256 (8 tiles) 24.2 / 18.5 / 18.2; 192 of 300 (10) 38.0 / 29.8 / 31.2, of 600 (19) 59.2 / 57.4 / 60.1; 32 of 128, 256 pairs, 5.2 / 5.2 / 5.3.  With 20
+    // queries a cache head, 8 / 2: 200 sequences of up to 250 54.4 / 40.6, 500 of up to 60 in float 127 / 80; 100 of up to 500, 8 / 4, 38.8 / 39.5.
     const int tiles = (a.max_len + C::kTile - 1) / C::kTile;
     if (tiles <= 2 || (many && tiles <= 8)) return launch_pairs<Core, DP, EXACT, 2>(a, s);
     if constexpr (C::kItemWaves > 4) {
