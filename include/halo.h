@@ -393,7 +393,7 @@ typedef struct {
 int halo_rope_table(int32_t n_pos, int32_t rotary_dim, double theta, float *table);
 
 /*
- * Appends N new tokens of any sequences to their caches, one launch.  Token i belongs to sequence seq[i] (seq NULL: to sequence i) and has position pos[i]:
+ * Appends N new tokens of any sequences to their caches, one launch (several from 2^24 tokens on).  Token i belongs to sequence seq[i] (seq NULL: to sequence i) and has position pos[i]:
  *   q_out[i] = R(pos[i]) q[i],   K row of the token = R(pos[i]) k[i],   V row of the token = v[i]
  * for every head, where R(p) turns the pairs (a, b) of a head's first rotary_dim elements by the angle of position p,
  *   (a, b) -> (a cos - b sin, b cos + a sin),
@@ -436,7 +436,7 @@ int halo_paged_attention(const halo_paged_shape *shape, int32_t T, const void *q
                          float scale, void *out, void *workspace, size_t ws_bytes, void *stream);
 
 /*
- * What stands between two blocks, one launch, one pass over the rows: the norm after a block with its gate, the scaled residual, the norm before the next block,
+ * What stands between two blocks, one launch (several from 2^22 rows on), one pass over the rows: the norm after a block with its gate, the scaled residual, the norm before the next block,
  *   u = post_norm ? n(y[t]) * w_post : y[t],   n(z) = z / sqrt(mean(z^2) + eps)
  *   h_out[t] = res_scale * h[t] + gate * u,    x[t] = n(h_out[t]) * w_pre
  * in float; h_out and x are each rounded once (x from the unrounded sum).
