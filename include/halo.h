@@ -436,6 +436,83 @@ int halo_paged_attention(const halo_paged_shape *shape, int32_t T, const void *q
                          float scale, void *out, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * The append for models that norm the heads of their queries and keys: as halo_paged_append, with
+ *   q_out[i] = R(pos[i]) n(q[i]) w_q,   K row of the token = R(pos[i]) n(k[i]) w_k,   n(z) = z / sqrt(mean(z^2) + eps)
+ * over each head's head_dim elements; values are moved as they are.  Computed in float, rounded once.
+ *   w_q, w_k [head_dim] dtype, one for all heads; NULL = 1.
+ * Errors: those of halo_paged_append; HALO_ERR_ARG also for eps negative or not finite, misaligned w_q, w_k.
+ */
+int halo_paged_append_norm(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                           const int32_t *page_table, const void *w_q, const void *w_k, float eps, const float *rope, int32_t rope_len,
+                           int32_t rotary_dim, int32_t rope_pairs, void *q_out, void *k_pages, void *v_pages, void *stream);
+
+/*
+ * A cache of eight-bit codes: pools k_codes, v_codes [n_pages][n_kv_heads][page_size][head_dim] int8 and k_scales, v_scales
+ * [n_pages][n_kv_heads][page_size] float in place of k_pages and v_pages (page tables, positions and pages that are none as above).  A row of a head,
+ * x, is kept as
+ *   s = max|x| / 127,   c = rint(x / s)   (ties to even; a row of zeros: s = 0, c = 0),
+ * the scale rounded to float (down, where 127 s would pass the largest one), and stands for s c.  A row with an infinity or NaN has s = NaN, c = 0: all of it stands for NaN.  dtype of the shape is that of
+ * queries and results.
+ *
+ * halo_paged_append_q8: halo_paged_append (qk_norm == 0; w_q, w_k and eps are then ignored) or halo_paged_append_norm (qk_norm != 0) into such a cache.  What becomes
+ * a code is computed in double up to its rounding, from the inputs and the table of angles as they are.  Errors: as theirs; HALO_ERR_ARG also for scales misaligned to 4 bytes.
+ *
+ * halo_paged_read_q8: what the rows of N tokens (pos, seq as in halo_paged_append) stand for, k_out, v_out [N][n_kv_heads][head_dim] dtype, computed in float; 0 for tokens that are padding.  Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N < 0, n_seq < 1, misaligned
+ * pointers), HALO_ERR_HIP.
+ *
+ * halo_paged_attention_q8: halo_paged_attention over such a cache (with halo_paged_workspace_bytes).  Products are of the codes themselves, a key's scale multiplies its score, a
+ * value's its probability; float queries and all probabilities enter the products as three bf16 values, which hold all of their bits.
+ */
+int halo_paged_append_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                         const int32_t *page_table, int32_t qk_norm, const void *w_q, const void *w_k, float eps, const float *rope,
+                         int32_t rope_len, int32_t rotary_dim, int32_t rope_pairs, void *q_out, int8_t *k_codes, float *k_scales,
+                         int8_t *v_codes, float *v_scales, void *stream);
+
+int halo_paged_read_q8(const halo_paged_shape *shape, int32_t N, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                       const int32_t *page_table, const int8_t *k_codes, const float *k_scales, const int8_t *v_codes,
+                       const float *v_scales, void *k_out, void *v_out, void *stream);
+
+int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const int8_t *k_codes,
+                            const float *k_scales, const int8_t *v_codes, const float *v_scales, const int32_t *page_table,
+                            const int32_t *lens, int32_t max_len, const uint8_t *mask, float scale, void *out, void *workspace,
+                            size_t ws_bytes, void *stream);
+
+/*
+ * Attention of chunks of new tokens of n_seq sequences over their pages (their own keys and values already appended): packed prompts, parts of prompts,
+ * drafted tokens to be looked over.  Rows starts[s] .. starts[s+1]-1 of q are the last tokens of sequence s, in order, and lens[s] counts its positions with them: the i-th of
+ * its n rows has position p = lens[s] - n + i and
+ *   out[row][h] = sum_j p_j V_j,   p = softmax_j(scale * q[row][h] . K_j),   j over positions 0 .. p
+ * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it).
+ *   q [N][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [N][n_heads][head_dim] dense
+ *   starts [n_seq + 1], non-decreasing, lens [n_seq], page_table [n_seq][max_pages] int32 on the device.  Rows before starts[0] and from starts[n_seq] on are
+ *       left as they are; a sequence may have none.  Rows outside 0 .. N-1 do not exist.
+ *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
+ *   mask [N][n_heads] uint8: a head whose byte is 0 gives out = 0; NULL = all survive.
+ * Positions in pages that are no pages count as absent; a row without positions (also: more rows than positions) gives out = 0; scores that are all -infinity give NaN.
+ * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16; float queries, keys, values and probabilities
+ * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (in keys and queries, floats from 2^128 (1 - 2^-9) on
+ * count as infinite, and an infinite one gives NaN).
+ * _q8: over a cache of codes, as halo_paged_attention_q8.
+ * How the work is cut depends on the arguments that the host sees and on the lengths; results do not depend on timing.
+ * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N outside 0..2^21, n_seq outside 0..4096, max_len, stride, alignment, scale not
+ * finite), HALO_ERR_WORKSPACE, HALO_ERR_HIP.  halo_paged_chunk_workspace_bytes: the workspace of up to N tokens of up to n_seq sequences; 0 for invalid
+ * arguments.
+ */
+size_t halo_paged_chunk_workspace_bytes(const halo_paged_shape *shape, int32_t N, int32_t n_seq);
+
+int halo_paged_chunk_attention(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k_pages,
+                               const void *v_pages, int32_t n_seq, const int32_t *starts, const int32_t *page_table,
+                               const int32_t *lens, int32_t max_len, const uint8_t *mask, float scale, void *out, void *workspace,
+                               size_t ws_bytes, void *stream);
+
+int halo_paged_chunk_attention_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const int8_t *k_codes,
+                                  const float *k_scales, const int8_t *v_codes, const float *v_scales, int32_t n_seq,
+                                  const int32_t *starts, const int32_t *page_table, const int32_t *lens, int32_t max_len,
+                                  const uint8_t *mask, float scale, void *out, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * What stands between two blocks, one launch (several from 2^22 rows on), one pass over the rows: the norm after a block with its gate, the scaled residual, the norm before the next block,
  *   u = post_norm ? n(y[t]) * w_post : y[t],   n(z) = z / sqrt(mean(z^2) + eps)
  *   h_out[t] = res_scale * h[t] + gate * u,    x[t] = n(h_out[t]) * w_pre

@@ -11,5 +11,7 @@ from .binding import (  # noqa: F401
     halo_group_sparse_ffn_q4, halo_ffn_forward_q4, halo_ffn_forward_ahead_q4,
     halo_profile_begin, halo_peak_read_stream, halo_peak_mfma_bf16, halo_stack_residual_norm,
     PagedShape, halo_rope_table, halo_paged_append, halo_paged_workspace_bytes, halo_paged_attention, halo_block_norm,
+    halo_paged_append_norm, halo_paged_append_q8, halo_paged_read_q8, halo_paged_attention_q8, halo_paged_chunk_workspace_bytes,
+    halo_paged_chunk_attention, halo_paged_chunk_attention_q8,
     halo_profile_end, halo_ratios_comp_greedy, halo_ratios_min_max, library_path, load_library, pack_down_proj, prepared,
 )

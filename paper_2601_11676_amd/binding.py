@@ -161,6 +161,21 @@ def load_library():
     lib.halo_paged_workspace_bytes.argtypes = [pp, i32]
     lib.halo_paged_attention.restype = C.c_int
     lib.halo_paged_attention.argtypes = [pp, i32, vp, i64, vp, vp, vp, vp, i32, vp, f32, vp, vp, sz, vp]
+    lib.halo_paged_append_norm.restype = C.c_int
+    lib.halo_paged_append_norm.argtypes = [pp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp, f32, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.halo_paged_append_q8.restype = C.c_int
+    lib.halo_paged_append_q8.argtypes = [pp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, i32, vp, vp, f32, vp, i32, i32, i32, vp, vp, vp, vp,
+                                         vp, vp]
+    lib.halo_paged_read_q8.restype = C.c_int
+    lib.halo_paged_read_q8.argtypes = [pp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.halo_paged_attention_q8.restype = C.c_int
+    lib.halo_paged_attention_q8.argtypes = [pp, i32, vp, i64, vp, vp, vp, vp, vp, vp, i32, vp, f32, vp, vp, sz, vp]
+    lib.halo_paged_chunk_workspace_bytes.restype = sz
+    lib.halo_paged_chunk_workspace_bytes.argtypes = [pp, i32, i32]
+    lib.halo_paged_chunk_attention.restype = C.c_int
+    lib.halo_paged_chunk_attention.argtypes = [pp, i32, vp, i64, vp, vp, i32, vp, vp, vp, i32, vp, f32, vp, vp, sz, vp]
+    lib.halo_paged_chunk_attention_q8.restype = C.c_int
+    lib.halo_paged_chunk_attention_q8.argtypes = [pp, i32, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, f32, vp, vp, sz, vp]
     lib.halo_block_norm.restype = C.c_int
     lib.halo_block_norm.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, f32, vp]
     lib.halo_profile_begin.restype = C.c_int
@@ -441,10 +456,18 @@ def _pool(t: torch.Tensor, shape: PagedShape):
     return _dense(t, shape.torch_dtype, shape.pool_elems)
 
 
-def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
-                      rope_pairs: bool = False, seq=None, stream=None) -> None:
-    """q [N][n_heads][head_dim] (or None, with q_out), k, v [N][n_kv_heads][head_dim]; rope as halo_rope_table gives it, on the
-    device; seq None: token i belongs to sequence i."""
+def _pool_q8(pool, shape: PagedShape):
+    """Addresses of a pool of codes and of its scales."""
+    codes, scales = pool
+    if codes.shape != shape.pool:
+        raise ValueError(f"pages are {list(shape.pool)}")
+    if scales.shape != shape.pool[:3]:
+        raise ValueError(f"scales are {list(shape.pool[:3])}")
+    return _dense(codes, torch.int8, shape.pool_elems), _dense(scales, torch.float32, shape.pool_elems // shape.head_dim)
+
+
+def _new_tokens(shape: PagedShape, q, k, v, pos, page_table, q_out, seq):
+    """What all appends take of their tokens: the arguments from N to page_table, and q_out's address."""
     dt, dim, n_kv = shape.torch_dtype, shape.head_dim, shape.n_kv_heads
     pk, sk, N = _heads(k, n_kv, dim, dt)
     pv, sv, Nv = _heads(v, n_kv, dim, dt)
@@ -458,18 +481,67 @@ def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pa
     n_seq = page_table.shape[0]
     if seq is None and n_seq < N:
         raise ValueError("without seq, every token needs a row of the page table")
-    pr, rows, half = None, 0, 0
-    if rope is not None:
-        rows, _, half = rope.shape
-        if not rows or not half:                     # without an address it would mean no rotation
-            raise ValueError("a table of angles has rows and columns")
-        pr = _dense(rope, torch.float32, rows * 2 * half)
-    rc = load_library().halo_paged_append(
-        shape.c, N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N),
-        n_seq, _dense(page_table, torch.int32, n_seq * shape.max_pages), pr, rows, 2 * half, 1 if rope_pairs else 0, po,
-        _pool(k_pages, shape), _pool(v_pages, shape), _stream(stream))
+    return (N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N), n_seq,
+            _dense(page_table, torch.int32, n_seq * shape.max_pages)), po
+
+
+def _angles(rope):
+    if rope is None:
+        return None, 0, 0
+    rows, _, half = rope.shape
+    if not rows or not half:                         # without an address it would mean no rotation
+        raise ValueError("a table of angles has rows and columns")
+    return _dense(rope, torch.float32, rows * 2 * half), rows, 2 * half
+
+
+def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
+                      rope_pairs: bool = False, seq=None, stream=None) -> None:
+    """q [N][n_heads][head_dim] (or None, with q_out), k, v [N][n_kv_heads][head_dim]; rope as halo_rope_table gives it, on the
+    device; seq None: token i belongs to sequence i."""
+    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
+    rc = load_library().halo_paged_append(shape.c, *new, *_angles(rope), 1 if rope_pairs else 0, po, _pool(k_pages, shape), _pool(v_pages, shape),
+                                          _stream(stream))
     if rc:
         raise HaloError("halo_paged_append", rc)
+
+
+def halo_paged_append_norm(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, w_q=None, w_k=None, eps: float = 1e-5,
+                           rope=None, rope_pairs: bool = False, seq=None, stream=None) -> None:
+    """halo_paged_append with the heads of queries and keys normed; w_q, w_k [head_dim] or None (1)."""
+    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
+    dt, dim = shape.torch_dtype, shape.head_dim
+    rc = load_library().halo_paged_append_norm(
+        shape.c, *new, None if w_q is None else _dense(w_q, dt, dim), None if w_k is None else _dense(w_k, dt, dim), eps, *_angles(rope),
+        1 if rope_pairs else 0, po, _pool(k_pages, shape), _pool(v_pages, shape), _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_append_norm", rc)
+
+
+def halo_paged_append_q8(shape: PagedShape, q, k, v, pos, page_table, k_pool, v_pool, q_out=None, qk_norm: bool = False, w_q=None, w_k=None,
+                         eps: float = 1e-5, rope=None, rope_pairs: bool = False, seq=None, stream=None) -> None:
+    """The append into a cache of codes: k_pool, v_pool are pairs (codes int8 [n_pages][n_kv_heads][page_size][head_dim], scales float32
+    [n_pages][n_kv_heads][page_size])."""
+    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
+    dt, dim = shape.torch_dtype, shape.head_dim
+    rc = load_library().halo_paged_append_q8(
+        shape.c, *new, 1 if qk_norm else 0, None if w_q is None else _dense(w_q, dt, dim), None if w_k is None else _dense(w_k, dt, dim), eps,
+        *_angles(rope), 1 if rope_pairs else 0, po, *_pool_q8(k_pool, shape), *_pool_q8(v_pool, shape), _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_append_q8", rc)
+
+
+def halo_paged_read_q8(shape: PagedShape, pos, page_table, k_pool, v_pool, k_out, v_out, seq=None, stream=None) -> None:
+    """What the rows of the tokens at positions pos [N] of sequences seq (None: token i of sequence i) stand for."""
+    N, n_seq = pos.numel(), page_table.shape[0]
+    if seq is None and n_seq < N:
+        raise ValueError("without seq, every token needs a row of the page table")
+    n = N * shape.n_kv_heads * shape.head_dim
+    rc = load_library().halo_paged_read_q8(
+        shape.c, N, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N), n_seq,
+        _dense(page_table, torch.int32, n_seq * shape.max_pages), *_pool_q8(k_pool, shape), *_pool_q8(v_pool, shape),
+        _dense(k_out, shape.torch_dtype, n), _dense(v_out, shape.torch_dtype, n), _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_read_q8", rc)
 
 
 def halo_paged_workspace_bytes(shape: PagedShape, T: int) -> int:
@@ -490,6 +562,54 @@ def halo_paged_attention(shape: PagedShape, q, k_pages, v_pages, page_table, len
         _dense(out, dt, T * shape.n_heads * shape.head_dim), _ptr(workspace), workspace.nbytes, _stream(stream))
     if rc:
         raise HaloError("halo_paged_attention", rc)
+
+
+def halo_paged_attention_q8(shape: PagedShape, q, k_pool, v_pool, page_table, lens, max_len: int, out, workspace, mask=None,
+                            scale: Optional[float] = None, stream=None) -> None:
+    """halo_paged_attention over a cache of codes: k_pool, v_pool are pairs (codes, scales) as in halo_paged_append_q8."""
+    dt = shape.torch_dtype
+    pq, sq, T = _heads(q, shape.n_heads, shape.head_dim, dt)
+    if scale is None:
+        scale = shape.head_dim ** -0.5
+    rc = load_library().halo_paged_attention_q8(
+        shape.c, T, pq, sq, *_pool_q8(k_pool, shape), *_pool_q8(v_pool, shape), _dense(page_table, torch.int32, T * shape.max_pages),
+        _dense(lens, torch.int32, T), max_len, None if mask is None else _dense(mask, torch.uint8, T * shape.n_heads), scale,
+        _dense(out, dt, T * shape.n_heads * shape.head_dim), _ptr(workspace), workspace.nbytes, _stream(stream))
+    if rc:
+        raise HaloError("halo_paged_attention_q8", rc)
+
+
+def halo_paged_chunk_workspace_bytes(shape: PagedShape, N: int, n_seq: int) -> int:
+    return int(load_library().halo_paged_chunk_workspace_bytes(shape.c, int(N), int(n_seq)))
+
+
+def _chunks(name, shape: PagedShape, q, pools, page_table, starts, lens, max_len, out, workspace, mask, scale, stream):
+    dt = shape.torch_dtype
+    pq, sq, N = _heads(q, shape.n_heads, shape.head_dim, dt)
+    n_seq = lens.numel()
+    if scale is None:
+        scale = shape.head_dim ** -0.5
+    rc = getattr(load_library(), name)(
+        shape.c, N, pq, sq, *pools, n_seq, _dense(starts, torch.int32, n_seq + 1), _dense(page_table, torch.int32, n_seq * shape.max_pages),
+        _dense(lens, torch.int32, n_seq), max_len, None if mask is None else _dense(mask, torch.uint8, N * shape.n_heads), scale,
+        _dense(out, dt, N * shape.n_heads * shape.head_dim), _ptr(workspace), workspace.nbytes, _stream(stream))
+    if rc:
+        raise HaloError(name, rc)
+
+
+def halo_paged_chunk_attention(shape: PagedShape, q, k_pages, v_pages, page_table, starts, lens, max_len: int, out, workspace, mask=None,
+                               scale: Optional[float] = None, stream=None) -> None:
+    """q [N][n_heads][head_dim], rows starts[s] .. starts[s + 1] - 1 (starts [n_seq + 1] int32) the last tokens of sequence s, lens [n_seq] with them;
+    scale None: 1 / sqrt(head_dim)."""
+    _chunks("halo_paged_chunk_attention", shape, q, (_pool(k_pages, shape), _pool(v_pages, shape)), page_table, starts, lens, max_len, out, workspace,
+            mask, scale, stream)
+
+
+def halo_paged_chunk_attention_q8(shape: PagedShape, q, k_pool, v_pool, page_table, starts, lens, max_len: int, out, workspace, mask=None,
+                                  scale: Optional[float] = None, stream=None) -> None:
+    """halo_paged_chunk_attention over a cache of codes: k_pool, v_pool are pairs (codes, scales) as in halo_paged_append_q8."""
+    _chunks("halo_paged_chunk_attention_q8", shape, q, (*_pool_q8(k_pool, shape), *_pool_q8(v_pool, shape)), page_table, starts, lens, max_len, out,
+            workspace, mask, scale, stream)
 
 
 def halo_block_norm(h, y, x, h_out=None, post_norm: bool = False, w_post=None, gate=None, res_scale: float = 1.0, w_pre=None,

@@ -1,0 +1,407 @@
+// New tokens' queries and keys normed head by head and rotated by their positions, keys and values written to the pages (halo_paged_append_norm), or as codes of
+// eight bits with a scale for each row of a head (halo_paged_append_q8); what such rows stand for (halo_paged_read_q8).
+//     n(z) = z / sqrt(mean(z^2) + eps) * w,  then  (a, b) -> (a cos - b sin, b cos + a sin)
+//     s = max|x| / 127,  c = rint(x / s),  standing for s c
+// Each element moves once and its row's sum or maximum is exchanged between the lanes that hold it, so bytes bound it; few tokens are a launch and two round trips.  A row of
+// a head is 2^n neighbouring lanes of a wave, two pieces of 16 bytes each (a head of 80 leaves lanes idle).
+//
+// A code is a decision: next to the border of two of them an error of the last bit moves the value by a whole step.  So what becomes a code is computed in double from
+// the inputs on (this card's double additions and products run at half the rate of float ones, and bytes still bound it); what does not, in float, rounded once.
+#include "../../include/halo.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "kernels.hpp"
+#include "paged_index.hpp"
+
+namespace halo {
+
+int check_paged_shape(const halo_paged_shape *s);
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct NormAppendArgs {
+    const void *q, *k, *v, *w_q, *w_k;
+    void *q_out, *k_pages, *v_pages;                 // pages of rows, or of codes
+    float *k_scales, *v_scales;
+    const int32_t *pos, *seq, *table;
+    const float *rope;
+    int64_t q_stride, k_stride, v_stride;
+    PagePool pool;
+    int n_heads, D, max_pages, n_seq, max_pos, rotary, pairs, norm;
+    int lanes;                                       // of a row
+    float eps;
+    int first;                                       // token of the launch's first workgroup
+};
+
+template <typename T> constexpr int kElems = 16 / (int)sizeof(T);
+
+template <typename T, typename C>
+__device__ __forceinline__ void load_piece(const T *p, C (&x)[kElems<T>])
+{
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+    if constexpr (sizeof(T) == 2) {
+        float f[8];
+        unpack8(v, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = f[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
+    }
+}
+
+template <bool PASS, typename T, typename C>
+__device__ __forceinline__ void store_piece(T *p, const C (&x)[kElems<T>])
+{
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2)
+            v[i] = (uint32_t)f32_to_bf16((float)x[2 * i]) | ((uint32_t)f32_to_bf16((float)x[2 * i + 1]) << 16);
+        else
+            v[i] = __float_as_uint((float)x[i]);
+    }
+    if constexpr (PASS)
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+    else
+        *reinterpret_cast<u32x4 *>(p) = v;
+}
+
+__device__ __forceinline__ float over_row(float v, int lanes)
+{
+    if (lanes > 1) v = xor_add<1>(v);
+    if (lanes > 2) v = xor_add<2>(v);
+    if (lanes > 4) v = xor_add<4>(v);
+    if (lanes > 8) v = xor_add<8>(v);
+    if (lanes > 16) v = xor_add<16>(v);
+    return v;
+}
+__device__ __forceinline__ double over_row(double v, int lanes)
+{
+    for (int d = 1; d < lanes; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+// Largest magnitude, by its bits: infinity and NaN are above every number.
+__device__ __forceinline__ double top_of_row(double v, int lanes)
+{
+    unsigned long long u = __double_as_longlong(fabs(v));
+    for (int d = 1; d < lanes; d <<= 1) u = max(u, (unsigned long long)__shfl_xor((long long)u, d));
+    return __longlong_as_double(u);
+}
+
+// A head's row in registers: pieces at elements e0 and e1 of lane `place`, normed and turned.
+template <typename T, typename C>
+struct HeadRow {
+    static constexpr int E = kElems<T>;
+    C x[E], y[E];
+
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = y[i] = (C)0;
+    }
+    __device__ __forceinline__ void load(const T *row, int e0, int e1)
+    {
+        load_piece(row + e0, x);
+        load_piece(row + e1, y);
+    }
+    __device__ __forceinline__ void norm(const NormAppendArgs &a, const T *w, int e0, int e1, bool in)
+    {
+        C sum = (C)0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) sum += x[i] * x[i] + y[i] * y[i];
+        const C by = (C)1 / sqrt(over_row(sum, a.lanes) / (C)a.D + (C)a.eps);
+        C u[E], v[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) u[i] = v[i] = (C)1;
+        if (w && in) {
+            load_piece(w + e0, u);
+            load_piece(w + e1, v);
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            x[i] = x[i] * by * u[i];
+            y[i] = y[i] * by * v[i];
+        }
+    }
+    __device__ __forceinline__ void turn(const NormAppendArgs &a, int pos, int e0, int e1, bool faced)
+    {
+        if (a.pairs) {
+            auto turn2 = [&](C (&z)[E], int e) {
+                if (e >= a.rotary) return;
+                const float *angles = a.rope + (int64_t)pos * a.rotary + e / 2;
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    const C cs = angles[i / 2], sn = angles[i / 2 + a.rotary / 2], p = z[i], r = z[i + 1];
+                    z[i] = p * cs - r * sn;
+                    z[i + 1] = r * cs + p * sn;
+                }
+            };
+            turn2(x, e0);
+            turn2(y, e1);
+        } else if (faced) {
+            const float *angles = a.rope + (int64_t)pos * a.rotary + e0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const C cs = angles[i], sn = angles[i + a.rotary / 2], p = x[i], r = y[i];
+                x[i] = p * cs - r * sn;
+                y[i] = r * cs + p * sn;
+            }
+        }
+    }
+    // as codes: what an exact quotient gives, also where the product with 127 / max falls next to the border of two
+    __device__ __forceinline__ void store_codes(int8_t *row, float *scale, int lanes, int e0, int e1, bool in, bool first) const
+    {
+        double top = 0.0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const unsigned long long u = __double_as_longlong(fabs((double)x[i])), v = __double_as_longlong(fabs((double)y[i]));
+            top = __longlong_as_double(max((unsigned long long)__double_as_longlong(top), max(u, v)));
+        }
+        top = top_of_row(top, lanes);
+        const bool number = top < (double)INFINITY;
+        const double step = top / 127.0, by = top > 0.0 && number ? 127.0 / top : 0.0;
+        auto code = [&](double z) {
+            const double w = z * by;
+            double c = rint(w);
+            if (fabs(w - c) > 0.5 - 1e-6) c = rint(z / step);
+            return (uint32_t)(uint8_t)(int8_t)(int)(number ? c : 0.0);
+        };
+        auto put = [&](const C (&z)[E], int e) {
+            uint32_t w[E / 4];
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i)
+                w[i] = code(z[4 * i]) | code(z[4 * i + 1]) << 8 | code(z[4 * i + 2]) << 16 | code(z[4 * i + 3]) << 24;
+            if (!in) return;
+            if constexpr (E == 8)
+                *reinterpret_cast<uint2 *>(row + e) = make_uint2(w[0], w[1]);
+            else
+                *reinterpret_cast<uint32_t *>(row + e) = w[0];
+        };
+        put(x, e0);
+        put(y, e1);
+        if (!first) return;
+        float s = number ? (float)step : NAN;
+        if (number && 127.0f * s == INFINITY) s = __uint_as_float(__float_as_uint(s) - 1);      // or the largest float would read back as infinity
+        *scale = s;
+    }
+};
+
+template <typename T, bool Q8, bool PASS>
+__global__ __launch_bounds__(kThreads) void append_norm_kernel(NormAppendArgs a)
+{
+    constexpr int E = kElems<T>;
+    const int token = a.first + blockIdx.x, places = a.D / (2 * E), at_once = kThreads / a.lanes;
+    const int place = threadIdx.x % a.lanes, row = threadIdx.x / a.lanes + blockIdx.y * at_once;
+    const int k_from = a.q ? a.n_heads : 0, v_from = k_from + a.pool.n_kv, rows = v_from + a.pool.n_kv;
+    const bool in = row < rows && place < places;    // the others stay for the exchanges
+
+    const int seq = a.seq ? a.seq[token] : token, pos = a.pos[token];
+    int page = -1;
+    if ((unsigned)seq < (unsigned)a.n_seq && (unsigned)pos < (unsigned)a.max_pos)
+        page = a.table[(int64_t)seq * a.max_pages + (pos >> a.pool.page_shift)];
+    const bool there = page_exists(a.pool, page);    // else padding: the same for the whole workgroup
+
+    // the two pieces of this place: with pairs that face each other, place p < rotary / (2 E) has p and the piece that faces it, the others share
+    // the rest of the head like this; else, and for values, piece p of either half of the head
+    const bool query = row < k_from, value = row >= v_from, facing = a.rope && !a.pairs && !value;
+    const int from = facing ? a.rotary : 0, p = facing ? place - a.rotary / (2 * E) : place;
+    const bool faced = facing && p < 0;
+    const int e0 = faced ? place * E : from + p * E, e1 = faced ? e0 + a.rotary / 2 : e0 + (a.D - from) / 2;
+
+    const int head = query ? row : row - (value ? v_from : k_from);
+    T *q_out = static_cast<T *>(a.q_out) + ((int64_t)token * a.n_heads + head) * a.D;
+    const T *source = query   ? static_cast<const T *>(a.q) + token * a.q_stride + head * a.D
+                      : value ? static_cast<const T *>(a.v) + token * a.v_stride + head * a.D
+                              : static_cast<const T *>(a.k) + token * a.k_stride + head * a.D;
+    if (!there) {
+        if (in && query) {
+            HeadRow<T, float> zero;
+            zero.zero();
+            store_piece<false>(q_out + e0, zero.x);
+            store_piece<false>(q_out + e1, zero.y);
+        }
+        return;
+    }
+    auto compute = [&](auto &r) {
+        r.zero();
+        if (in) r.load(source, e0, e1);
+        if (a.norm) {
+            auto normed = r;
+            normed.norm(a, static_cast<const T *>(query ? a.w_q : a.w_k), e0, e1, in && !value);
+            if (!value) r = normed;
+        }
+        if (a.rope && !value && in) r.turn(a, pos, e0, e1, faced);
+    };
+    const int64_t cell = paged_row(a.pool, page, head, pos);
+    if constexpr (Q8) {
+        HeadRow<T, double> r;
+        compute(r);
+        if (query && in) {
+            store_piece<PASS>(q_out + e0, r.x);
+            store_piece<PASS>(q_out + e1, r.y);
+        }
+        r.store_codes(static_cast<int8_t *>(value ? a.v_pages : a.k_pages) + cell * a.D, (value ? a.v_scales : a.k_scales) + cell, a.lanes, e0, e1,
+                      in && !query, in && !query && place == 0);
+    } else {
+        HeadRow<T, float> r;
+        compute(r);
+        T *to = query ? q_out : static_cast<T *>(value ? a.v_pages : a.k_pages) + cell * a.D;
+        if (in) {
+            store_piece<PASS>(to + e0, r.x);
+            store_piece<PASS>(to + e1, r.y);
+        }
+    }
+}
+
+struct ReadArgs {
+    const int8_t *k_codes, *v_codes;
+    const float *k_scales, *v_scales;
+    const int32_t *pos, *seq, *table;
+    void *k_out, *v_out;
+    PagePool pool;
+    int D, max_pages, n_seq, first;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void read_q8_kernel(ReadArgs a)
+{
+    constexpr int E = kElems<T>;
+    const int token = a.first + blockIdx.x, unit = blockIdx.y * kThreads + threadIdx.x, row_units = a.D / E, units = a.pool.n_kv * row_units;
+    if (unit >= 2 * units) return;
+    const bool value = unit >= units;
+    const int u = value ? unit - units : unit, head = u / row_units, e = (u - head * row_units) * E;
+    const int seq = a.seq ? a.seq[token] : token, pos = a.pos[token];
+    int page = -1;
+    if ((unsigned)seq < (unsigned)a.n_seq && (unsigned)pos < (unsigned)(a.max_pages << a.pool.page_shift))
+        page = a.table[(int64_t)seq * a.max_pages + (pos >> a.pool.page_shift)];
+    const int64_t cell = paged_row(a.pool, page, head, pos);
+    float x[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = 0.0f;
+    if (cell >= 0) {
+        const float s = (value ? a.v_scales : a.k_scales)[cell];
+        const int8_t *c = (value ? a.v_codes : a.k_codes) + cell * a.D + e;
+        uint32_t w[E / 4];
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) w[i] = reinterpret_cast<const uint32_t *>(c)[i];
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = s * (float)(int8_t)(w[i / 4] >> (8 * (i % 4)));
+    }
+    store_piece<false>(static_cast<T *>(value ? a.v_out : a.k_out) + ((int64_t)token * a.pool.n_kv + head) * a.D + e, x);
+}
+
+bool off(const void *p, unsigned by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; }
+
+// tokens whose workgroups number less than 2^32 threads
+constexpr int64_t kRun = 0xffffffffu / kThreads;
+
+int append(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+           const int32_t *pos, const int32_t *seq, int32_t n_seq, const int32_t *table, int32_t norm, const void *w_q, const void *w_k, float eps,
+           const float *rope, int32_t rope_len, int32_t rotary_dim, int32_t rope_pairs, void *q_out, void *k_pages, float *k_scales, void *v_pages,
+           float *v_scales, bool codes, void *stream)
+{
+    if (const int rc = check_paged_shape(shape)) return rc;
+    if (N < 0) return HALO_ERR_ARG;
+    if (N == 0) return HALO_OK;
+    if (!k || !v || !pos || !table || !k_pages || !v_pages || !q != !q_out || (codes && (!k_scales || !v_scales))) return HALO_ERR_NULL;
+    const halo_paged_shape &s = *shape;
+    const int size = s.dtype == HALO_F32 ? 4 : 2;
+    auto bad_stride = [&](int64_t stride, int heads) { return stride < (int64_t)heads * s.head_dim || stride * size % 16; };
+    if (n_seq < 1 || (q && (q == q_out || bad_stride(q_stride, s.n_heads))) || bad_stride(k_stride, s.n_kv_heads) ||
+        bad_stride(v_stride, s.n_kv_heads))
+        return HALO_ERR_ARG;
+    if (off(q, 16) || off(k, 16) || off(v, 16) || off(q_out, 16) || off(k_pages, 16) || off(v_pages, 16) || off(rope, 16) || off(pos, 4) ||
+        off(seq, 4) || off(table, 4) || off(k_scales, 4) || off(v_scales, 4))
+        return HALO_ERR_ARG;
+    if (norm && (off(w_q, 16) || off(w_k, 16) || !(eps >= 0.0f) || !std::isfinite(eps))) return HALO_ERR_ARG;
+    if (rope && (rope_len < 1 || rotary_dim < 16 || rotary_dim % 16 || rotary_dim > s.head_dim)) return HALO_ERR_ARG;
+
+    NormAppendArgs a{};
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages; a.k_scales = k_scales; a.v_scales = v_scales;
+    a.w_q = norm ? w_q : nullptr; a.w_k = norm ? w_k : nullptr; a.norm = norm != 0; a.eps = eps;
+    a.pos = pos; a.seq = seq; a.table = table; a.rope = rope;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
+    a.n_heads = s.n_heads; a.D = s.head_dim; a.max_pages = s.max_pages; a.n_seq = n_seq;
+    a.max_pos = s.max_pages * s.page_size;
+    if (rope && rope_len < a.max_pos) a.max_pos = rope_len;
+    a.rotary = rope ? rotary_dim : 0;
+    a.pairs = rope_pairs != 0;
+    a.lanes = 1;
+    while (a.lanes * 32 < s.head_dim * size) a.lanes *= 2;
+    const int at_once = kThreads / a.lanes, rows = (q ? s.n_heads : 0) + 2 * s.n_kv_heads;
+    // stores with the non-temporal hint where they fill whole 64-byte parts of lines and are many, as in paged_append.hip
+    const int faced = rope && !rope_pairs ? rotary_dim : 0;
+    const bool runs = (faced / 2 * size | (s.head_dim - faced) / 2 * size | s.head_dim / 2 * size) % 64 == 0;
+    const bool pass = runs && (int64_t)N * rows * s.head_dim * size >= (4 << 20);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    for (int64_t first = 0; first < N; first += kRun) {
+        a.first = (int)first;
+        const dim3 grid((unsigned)std::min(kRun, N - first), (rows + at_once - 1) / at_once), threads(kThreads);
+        auto launch = [&](auto kernel) { kernel<<<grid, threads, 0, st>>>(a); };
+        if (s.dtype == HALO_F32) {
+            if (codes) launch(pass ? append_norm_kernel<float, true, true> : append_norm_kernel<float, true, false>);
+            else launch(pass ? append_norm_kernel<float, false, true> : append_norm_kernel<float, false, false>);
+        } else {
+            if (codes) launch(pass ? append_norm_kernel<bf16_t, true, true> : append_norm_kernel<bf16_t, true, false>);
+            else launch(pass ? append_norm_kernel<bf16_t, false, true> : append_norm_kernel<bf16_t, false, false>);
+        }
+    }
+    return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace halo
+
+extern "C" int halo_paged_append_norm(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                      const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                                      const int32_t *page_table, const void *w_q, const void *w_k, float eps, const float *rope, int32_t rope_len,
+                                      int32_t rotary_dim, int32_t rope_pairs, void *q_out, void *k_pages, void *v_pages, void *stream)
+{
+    return halo::append(shape, N, q, q_stride, k, k_stride, v, v_stride, pos, seq, n_seq, page_table, 1, w_q, w_k, eps, rope, rope_len, rotary_dim, rope_pairs,
+                        q_out, k_pages, nullptr, v_pages, nullptr, false, stream);
+}
+
+extern "C" int halo_paged_append_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                    const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                                    const int32_t *page_table, int32_t qk_norm, const void *w_q, const void *w_k, float eps, const float *rope,
+                                    int32_t rope_len, int32_t rotary_dim, int32_t rope_pairs, void *q_out, int8_t *k_codes, float *k_scales,
+                                    int8_t *v_codes, float *v_scales, void *stream)
+{
+    return halo::append(shape, N, q, q_stride, k, k_stride, v, v_stride, pos, seq, n_seq, page_table, qk_norm, w_q, w_k, eps, rope, rope_len, rotary_dim,
+                        rope_pairs, q_out, k_codes, k_scales, v_codes, v_scales, true, stream);
+}
+
+extern "C" int halo_paged_read_q8(const halo_paged_shape *shape, int32_t N, const int32_t *pos, const int32_t *seq, int32_t n_seq,
+                                  const int32_t *page_table, const int8_t *k_codes, const float *k_scales, const int8_t *v_codes,
+                                  const float *v_scales, void *k_out, void *v_out, void *stream)
+{
+    using namespace halo;
+    if (const int rc = check_paged_shape(shape)) return rc;
+    if (N < 0) return HALO_ERR_ARG;
+    if (N == 0) return HALO_OK;
+    if (!pos || !page_table || !k_codes || !k_scales || !v_codes || !v_scales || !k_out || !v_out) return HALO_ERR_NULL;
+    if (n_seq < 1 || off(k_codes, 16) || off(v_codes, 16) || off(k_out, 16) || off(v_out, 16) || off(k_scales, 4) || off(v_scales, 4) || off(pos, 4) ||
+        off(seq, 4) || off(page_table, 4))
+        return HALO_ERR_ARG;
+    const halo_paged_shape &s = *shape;
+    ReadArgs a{};
+    a.k_codes = k_codes; a.v_codes = v_codes; a.k_scales = k_scales; a.v_scales = v_scales;
+    a.pos = pos; a.seq = seq; a.table = page_table; a.k_out = k_out; a.v_out = v_out;
+    a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
+    a.D = s.head_dim; a.max_pages = s.max_pages; a.n_seq = n_seq;
+    const int units = 2 * s.n_kv_heads * s.head_dim / (s.dtype == HALO_F32 ? 4 : 8);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    for (int64_t first = 0; first < N; first += kRun) {
+        a.first = (int)first;
+        const dim3 grid((unsigned)std::min(kRun, N - first), (units + kThreads - 1) / kThreads), threads(kThreads);
+        if (s.dtype == HALO_F32) read_q8_kernel<float><<<grid, threads, 0, st>>>(a);
+        else read_q8_kernel<bf16_t><<<grid, threads, 0, st>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
+}

@@ -34,9 +34,9 @@ inline int rows_of_unit(const halo_paged_shape &s, int most)
 inline int most_rows(const halo_paged_shape &s) { return s.head_dim <= 128 ? 2 * kCols : kCols; }
 
 // Bytes of a call's cache, as far as the host knows.
-inline int64_t most_bytes(const halo_paged_shape &s, int T, int max_len)
+inline int64_t most_bytes(const halo_paged_shape &s, int T, int max_len, bool codes)
 {
-    return (int64_t)T * s.n_kv_heads * max_len * s.head_dim * 2 * (s.dtype == HALO_F32 ? 4 : 2);
+    return (int64_t)T * s.n_kv_heads * max_len * 2 * (codes ? s.head_dim + 4 : s.head_dim * (s.dtype == HALO_F32 ? 4 : 2));
 }
 
 struct PagedWorkspace {
@@ -75,27 +75,30 @@ extern "C" size_t halo_paged_workspace_bytes(const halo_paged_shape *shape, int3
     return PagedWorkspace(*shape, T).bytes;
 }
 
-extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const void *k_pages,
-                                    const void *v_pages, const int32_t *page_table, const int32_t *lens, int32_t max_len,
-                                    const uint8_t *mask, float scale, void *out, void *workspace, size_t ws_bytes, void *stream)
+namespace halo {
+namespace {
+
+int attend(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const void *k, const float *k_scale, const void *v, const float *v_scale,
+           bool codes, const int32_t *page_table, const int32_t *lens, int32_t max_len, const uint8_t *mask, float scale, void *out, void *workspace,
+           size_t ws_bytes, void *stream)
 {
-    using namespace halo;
     if (const int rc = check_paged_shape(shape)) return rc;
     if (T < 0 || T > kMaxSeqs) return HALO_ERR_ARG;
     if (T == 0) return HALO_OK;
-    if (!q || !k_pages || !v_pages || !page_table || !lens || !out) return HALO_ERR_NULL;
+    if (!q || !k || !v || !page_table || !lens || !out || (codes && (!k_scale || !v_scale))) return HALO_ERR_NULL;
     const halo_paged_shape &s = *shape;
     const int size = s.dtype == HALO_F32 ? 4 : 2;
     auto odd = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; };
     if (max_len < 1 || max_len > s.max_pages * s.page_size || !std::isfinite(scale)) return HALO_ERR_ARG;
-    if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q) || odd(k_pages) || odd(v_pages) || odd(out) ||
-        odd(workspace) || (reinterpret_cast<uintptr_t>(page_table) & 3u) || (reinterpret_cast<uintptr_t>(lens) & 3u))
+    if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q) || odd(k) || odd(v) || odd(out) ||
+        odd(workspace) || (reinterpret_cast<uintptr_t>(page_table) & 3u) || (reinterpret_cast<uintptr_t>(lens) & 3u) ||
+        ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u))
         return HALO_ERR_ARG;
     const PagedWorkspace ws(s, T);
     if (!workspace || ws_bytes < ws.bytes) return HALO_ERR_WORKSPACE;
 
     AttendArgs a{};
-    a.q = q; a.k = k_pages; a.v = v_pages; a.table = page_table; a.lens = lens; a.mask = mask; a.out = out;
+    a.q = q; a.k = k; a.v = v; a.k_scale = k_scale; a.v_scale = v_scale; a.table = page_table; a.lens = lens; a.mask = mask; a.out = out;
     char *w = static_cast<char *>(workspace);
     a.plan = reinterpret_cast<int32_t *>(w + ws.plan);
     a.stats = reinterpret_cast<float *>(w + ws.stats);
@@ -103,18 +106,39 @@ extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, co
     a.q_stride = q_stride;
     a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
     a.T = T; a.n_heads = s.n_heads; a.group = s.n_heads / s.n_kv_heads;
-    a.bytes = most_bytes(s, T, max_len);
+    a.bytes = most_bytes(s, T, max_len, codes);
     // More than 16 queries a cache head: 32 at once read the cache once, 16 at a time have more workgroups.  us, 32 / 16, lengths from half of the longest on: 16 sequences of up to
     // 8000, 8 cache heads with 20 queries (524 MB at the longest) 77 / 134; 30 of up to 5000, 2 with 20, heads of 96 (115 MB) 27.5 / 36.7; 8 of up to 700, 2 with 20 (6 MB)
     // 12.3 / 8.3.  Float, 8 cache heads with 20 queries: 24 of up to 5000 150 / 243; 4 of up to 4000 (131 MB) 31.8 / 40.6; 4 of up to 1000 (33 MB) 20.6 / 20.2; 1 of 1000
     // 18.8 / 14.4.
-    a.rows = rows_of_unit(s, a.bytes > (64 << 20) ? most_rows(s) : kCols);
+    a.rows = rows_of_unit(s, a.bytes > (64 << 20) && !(codes && s.dtype == HALO_F32) ? most_rows(s) : kCols);
     a.n_qt = (a.group + a.rows - 1) / a.rows;
     a.n_units = s.n_kv_heads * a.n_qt;
     a.D = s.head_dim; a.max_pages = s.max_pages; a.max_len = max_len;
     a.scale2 = scale * 1.44269504088896341f;
     if ((int64_t)((max_len + 15) / 16) * T * a.n_units > (1 << 30)) return HALO_ERR_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (codes) return s.dtype == HALO_F32 ? launch_attend_q8_f32(a, st) : a.rows <= kCols ? launch_attend_q8(a, st) : launch_attend_q8_32(a, st);
     if (s.dtype == HALO_BF16) return a.rows <= kCols ? launch_attend_bf16(a, st) : launch_attend_bf16_32(a, st);
     return a.rows <= 4 ? launch_attend_f32_4(a, st) : a.rows <= kCols ? launch_attend_f32(a, st) : launch_attend_f32_32(a, st);
+}
+
+}  // namespace
+}  // namespace halo
+
+extern "C" int halo_paged_attention(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const void *k_pages,
+                                    const void *v_pages, const int32_t *page_table, const int32_t *lens, int32_t max_len,
+                                    const uint8_t *mask, float scale, void *out, void *workspace, size_t ws_bytes, void *stream)
+{
+    return halo::attend(shape, T, q, q_stride, k_pages, nullptr, v_pages, nullptr, false, page_table, lens, max_len, mask, scale, out, workspace, ws_bytes,
+                        stream);
+}
+
+extern "C" int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void *q, int64_t q_stride, const int8_t *k_codes,
+                                       const float *k_scales, const int8_t *v_codes, const float *v_scales, const int32_t *page_table,
+                                       const int32_t *lens, int32_t max_len, const uint8_t *mask, float scale, void *out, void *workspace,
+                                       size_t ws_bytes, void *stream)
+{
+    return halo::attend(shape, T, q, q_stride, k_codes, k_scales, v_codes, v_scales, true, page_table, lens, max_len, mask, scale, out, workspace, ws_bytes,
+                        stream);
 }

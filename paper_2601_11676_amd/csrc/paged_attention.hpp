@@ -12,6 +12,7 @@ namespace halo {
 
 struct AttendArgs {
     const void *q, *k, *v;
+    const float *k_scale, *v_scale;                  // of a cache of codes: one for each row
     const int32_t *table, *lens;
     const uint8_t *mask;
     void *out;
@@ -56,6 +57,8 @@ __device__ __forceinline__ V row_load(__amdgpu_buffer_rsrc_t rows, uint32_t at)
 {
     if constexpr (sizeof(V) == 16)
         return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, POLICY));
+    else if constexpr (sizeof(V) == 4)
+        return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, POLICY));
     else
         return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, POLICY));
 }
@@ -78,7 +81,7 @@ struct KeyPlace {
     {
         const int row = lane / kPieces, piece = lane % kPieces, c = lane & 15, g = lane >> 4;
         from = piece * 16 < D * (int)sizeof(Elem) ? (uint32_t)(row * D * (int)sizeof(Elem) + piece * 16) : kOutOfRange;
-        in = row * kBytes + ((piece ^ row) << 4);
+        in = row * kBytes + ((piece ^ (row & kTurn)) << 4);
         out = c * kBytes + ((g ^ (c & kTurn)) << 4);
     }
     __device__ __forceinline__ uint32_t put(int i) const { return (in ^ ((i * kRows & kTurn) << 4)) + i * kRows * kBytes; }
@@ -115,7 +118,8 @@ __device__ __forceinline__ void turn_keys(Core &core)
 // The running softmax of one unit over bf16 rows, kSub times 16 tokens a step.  DP = head dimension, or the next of 64, 128, 256 above it (EXACT false).
 template <int DP, bool EXACT, int HINT, int TILES>
 struct CoreBf16 {
-    typedef bf16_t Elem;
+    typedef bf16_t Elem, Cell;                          // queries and results; the cache
+    static constexpr bool kScaled = false;
     static constexpr int QT = TILES;                 // times 16 queries: more than one where a cache head has more than 16
     static constexpr int kSub = DP > 64 ? 2 : 4, kTile = kSub * 16;      // rows of 128 and 64: 16 KiB of keys and values a step
     static constexpr int kItemWaves = DP > 128 ? 4 : 8;     // waves of a workgroup that takes a pair: rows of 256 need more than 256 registers
@@ -273,7 +277,8 @@ template <int DP, bool EXACT, int HINT> using CoreBf16Two = CoreBf16<DP, EXACT, 
 // takes a pair has eight waves here too, which spill 9 registers with heads of 80 to 112.
 template <int DP, bool EXACT, int HINT, int TILES>
 struct CoreF32 {
-    typedef float Elem;
+    typedef float Elem, Cell;                          // queries and results; the cache
+    static constexpr bool kScaled = false;
     static constexpr int QT = TILES;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
     static constexpr int kSteps = 4, kLeast = DP > 128 ? 4 : 2;
@@ -392,7 +397,8 @@ template <int DP, bool EXACT, int HINT> using CoreF32Two = CoreF32<DP, EXACT, HI
 // where lane l = (g, m, j) = (l >> 4, l >> 2 & 3, l & 3), j its row of an operand and its column, a query, of the other and of the results.
 template <int DP, bool EXACT, int HINT>
 struct CoreF32Few {
-    typedef float Elem;
+    typedef float Elem, Cell;                          // queries and results; the cache
+    static constexpr bool kScaled = false;
     static constexpr int QT = 1;
     static constexpr int kSub = DP > 64 ? 1 : 2, kTile = kSub * 16;
     static constexpr int kSteps = DP > 128 ? 8 : 6, kLeast = DP > 128 ? 4 : 2;
@@ -497,6 +503,198 @@ struct CoreF32Few {
     }
 };
 
+// The running softmax over rows of eight-bit codes c with a scale s each, a row standing for s c.  A code is a bf16 number, so that the matrix cores take products of
+// codes exactly; a key's scale multiplies its score, a value's the probability that goes into the product.  Queries are QP bf16 parts (three hold a float),
+// probabilities three.  A lane's piece of a key is 16 elements, which are two operands.
+template <typename T, int DP, bool EXACT, int HINT, int TILES, int QP>
+struct CoreQ8 {
+    typedef T Elem;
+    typedef int8_t Cell;
+    static constexpr bool kScaled = true;
+    static constexpr int QT = TILES;
+    static constexpr int kSub = DP > 128 ? 2 : 4, kTile = kSub * 16;
+    static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 || (DP > 64 && QT * QP > 1) ? 1 : 2;
+    static constexpr int kSteps = DP > 64 ? 8 : 4, kLeast = DP > 128 ? 4 : 2;
+    static constexpr int kMostRows = QT * kCols * DP * 4, kStage = kTile * DP > kMostRows ? kTile * DP : kMostRows;
+    static constexpr int KS = DP / 64;               // pieces of a key row in a lane
+    static constexpr int VEC = DP > 64 ? 8 : 4, VH = DP > 128 ? 2 : 1, kAcc = VEC * VH;
+    typedef std::conditional_t<VEC == 8, u32x2, uint32_t> VPiece;
+
+    u32x4 qf[QT][QP][2 * KS], kf[kSub][KS];
+    VPiece vf[4 * kSub][VH];
+    f32x4 acc[QT][kAcc], ks[kSub], vs[kSub];
+    float m[QT], l[QT];
+    KeyPlace<int8_t, DP> keys;
+    char *lds;
+    uint32_t voff[VH];
+    int D, c, g;
+
+    __device__ __forceinline__ void place(int d, int lane, char *own)
+    {
+        D = EXACT ? DP : d;
+        c = lane & 15;
+        g = lane >> 4;
+        lds = own;
+        keys.place(D, lane);
+#pragma unroll
+        for (int h = 0; h < VH; ++h) {
+            const int dim = h * 16 * VEC + c * VEC;
+            voff[h] = EXACT || dim < D ? (uint32_t)(g * 4 * D + dim) : kOutOfRange;
+        }
+    }
+    __device__ __forceinline__ void begin(const Elem *q, int nq)
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+#pragma unroll
+            for (int s = 0; s < 2 * KS; ++s) {
+                const int n = min(t * kCols + c, nq - 1), dim = (s / 2 * 4 + g) * 16 + s % 2 * 8;
+                const bool in = EXACT || dim < D;
+                float x[8];
+                load8(q + n * D + (in ? dim : 0), x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float a = in ? x[2 * i] : 0.0f, b = in ? x[2 * i + 1] : 0.0f;
+#pragma unroll
+                    for (int p = 0; p < QP; ++p) {
+                        qf[t][p][s][i] = pair(a, b);
+                        a -= bf16_lo(qf[t][p][s][i]);
+                        b -= bf16_hi(qf[t][p][s][i]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            l[t] = 0.0f;
+            m[t] = -INFINITY;
+        }
+    }
+    static __device__ __forceinline__ uint32_t pair(float a, float b)
+    {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    }
+    // byte i of a word as a float
+    static __device__ __forceinline__ float number(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+    // the upper halves of two floats that are bf16 numbers
+    static __device__ __forceinline__ uint32_t upper(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
+    __device__ __forceinline__ void load_k(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[i][s] = row_load<u32x4, HINT == kPassBoth ? kNt : 0>(rows[i], keys.from + s * keys.kRows * D);
+    }
+    __device__ __forceinline__ void load_v(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < 4 * kSub; ++i)
+#pragma unroll
+            for (int h = 0; h < VH; ++h) vf[i][h] = row_load<VPiece, HINT != kKeepAll ? kNt : 0>(rows[i >> 2], voff[h] + (i & 3) * D);
+    }
+    __device__ __forceinline__ void load_k_scales(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) ks[i] = row_load<f32x4, 0>(rows[i], g * 16);
+    }
+    __device__ __forceinline__ void load_v_scales(const __amdgpu_buffer_rsrc_t (&rows)[kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) vs[i] = row_load<f32x4, 0>(rows[i], g * 16);
+    }
+    static __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &acc)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    }
+    __device__ __forceinline__ void scores(float (&x)[QT][4 * kSub])
+    {
+        turn_keys(*this);
+        f32x4 s[QT][kSub];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < kSub; ++i) s[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 2 * KS; ++k)
+#pragma unroll
+            for (int i = 0; i < kSub; ++i) {
+                u32x4 a;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t codes = kf[i][k / 2][k % 2 * 2 + w / 2];
+                    a[w] = upper(number(codes, w % 2 * 2), number(codes, w % 2 * 2 + 1));
+                }
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int p = 0; p < QP; ++p) s[t][i] = mfma(a, qf[t][p][k], s[t][i]);
+            }
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4 * kSub; ++e) x[t][e] = s[t][e >> 2][e & 3] * ks[e >> 2][e & 3];
+    }
+    __device__ __forceinline__ void rescale(int t, float by)
+    {
+#pragma unroll
+        for (int j = 0; j < kAcc; ++j) acc[t][j] *= by;
+        l[t] *= by;
+    }
+    __device__ __forceinline__ void accumulate(const float (&p)[QT][4 * kSub])
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4 * kSub; i += 4) l[t] += (p[t][i] + p[t][i + 1]) + (p[t][i + 2] + p[t][i + 3]);
+#pragma unroll
+        for (int o = 0; o < 4 * kSub; o += 8) {
+            u32x4 part[QT][3];
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int e = o + 2 * t;
+                    float a = p[q][e] * vs[e >> 2][e & 3], b = p[q][e + 1] * vs[e >> 2][(e & 3) + 1];
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+                        part[q][i][t] = pair(a, b);
+                        a -= bf16_lo(part[q][i][t]);
+                        b -= bf16_hi(part[q][i][t]);
+                    }
+                }
+#pragma unroll
+            for (int h = 0; h < VH; ++h)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    auto value = [&](int e) {
+                        if constexpr (VEC == 8) return number(vf[e][h][j >> 2], j & 3);
+                        else return number(vf[e][h], j);
+                    };
+                    u32x4 a;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) a[t] = upper(value(o + 2 * t), value(o + 2 * t + 1));
+#pragma unroll
+                    for (int q = 0; q < QT; ++q)
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) acc[q][h * VEC + j] = mfma(a, part[q][i], acc[q][h * VEC + j]);
+                }
+        }
+    }
+    __device__ __forceinline__ int col() const { return c; }
+    __device__ __forceinline__ int row() const { return g * 4; }
+    __device__ __forceinline__ bool stores() const { return true; }
+    __device__ __forceinline__ float top(float v) const { return xor_max16_32(v); }
+    __device__ __forceinline__ void finish(float (&out)[QT])
+    {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) out[t] = xor_add<16>(xor_add<32>(l[t]));
+    }
+};
+
+template <int DP, bool EXACT, int HINT> using CoreQ8One = CoreQ8<bf16_t, DP, EXACT, HINT, 1, 1>;
+template <int DP, bool EXACT, int HINT> using CoreQ8Two = CoreQ8<bf16_t, DP, EXACT, HINT, 2, 1>;
+template <int DP, bool EXACT, int HINT> using CoreQ8Float = CoreQ8<float, DP, EXACT, HINT, 1, 3>;
+
 // The tiles first, first + stride, .. (count of them) of one sequence that a wave takes, and the pages of their 16-token parts: 64 parts at a time, one
 // a lane.  All calls are wave-uniform.
 template <typename Core>
@@ -524,12 +722,13 @@ struct Tiles {
 template <typename Core>
 struct Step {
     __amdgpu_buffer_rsrc_t k[Core::kSub], v[Core::kSub];
+    __amdgpu_buffer_rsrc_t ks[Core::kScaled ? Core::kSub : 1], vs[Core::kScaled ? Core::kSub : 1];
     int live[Core::kSub];                            // tokens of the 16 that count
     bool whole, any;
 
     __device__ __forceinline__ Step(const AttendArgs &a, Tiles<Core> &tiles, int kv, int len, int i)
     {
-        constexpr int kBytes = sizeof(typename Core::Elem);
+        constexpr int kBytes = sizeof(typename Core::Cell);
         if (i - tiles.from >= Tiles<Core>::kHeld) tiles.fetch(i);
         whole = true;
         any = false;
@@ -544,6 +743,12 @@ struct Step {
             const uint64_t at = (uint64_t)(uint32_t)same((int)(bytes >> 32)) << 32 | (uint32_t)same((int)bytes);
             k[p] = buffer_of(static_cast<const char *>(a.k) + at, live[p] * a.D * kBytes);
             v[p] = buffer_of(static_cast<const char *>(a.v) + at, live[p] * a.D * kBytes);
+            if constexpr (Core::kScaled) {
+                const uint64_t from = (uint64_t)(row < 0 ? 0 : row) * 4;
+                const uint64_t scale = (uint64_t)(uint32_t)same((int)(from >> 32)) << 32 | (uint32_t)same((int)from);
+                ks[p] = buffer_of(reinterpret_cast<const char *>(a.k_scale) + scale, live[p] * 4);
+                vs[p] = buffer_of(reinterpret_cast<const char *>(a.v_scale) + scale, live[p] * 4);
+            }
         }
     }
 };
@@ -579,6 +784,19 @@ __device__ __forceinline__ void softmax_step(Core &core, const Step<Core> &st, f
     }
 }
 
+template <typename Core>
+__device__ __forceinline__ void load_keys(Core &core, const Step<Core> &st)
+{
+    core.load_k(st.k);
+    if constexpr (Core::kScaled) core.load_k_scales(st.ks);
+}
+template <typename Core>
+__device__ __forceinline__ void load_values(Core &core, const Step<Core> &st)
+{
+    core.load_v(st.v);
+    if constexpr (Core::kScaled) core.load_v_scales(st.vs);
+}
+
 // `count` tiles of a sequence against the queries in `core`: the next step's keys are asked for as soon as this one's are used up, and its
 // values after this one's.
 template <typename Core>
@@ -586,15 +804,15 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, Core &core, Ti
 {
     float x[Core::QT][4 * Core::kSub];
     Step<Core> now(a, tiles, kv, len, 0);
-    core.load_k(now.k);
-    core.load_v(now.v);
+    load_keys(core, now);
+    load_values(core, now);
     for (int i = 1; i < count; ++i) {
         const Step<Core> next(a, tiles, kv, len, i);
         core.scores(x);
-        core.load_k(next.k);
+        load_keys(core, next);
         softmax_step(core, now, a.scale2, x);
         core.accumulate(x);
-        core.load_v(next.v);
+        load_values(core, next);
         now = next;
     }
     core.scores(x);
@@ -1121,5 +1339,9 @@ int launch_attend_bf16_32(const AttendArgs &a, hipStream_t s);
 int launch_attend_f32_4(const AttendArgs &a, hipStream_t s);
 int launch_attend_f32(const AttendArgs &a, hipStream_t s);
 int launch_attend_f32_32(const AttendArgs &a, hipStream_t s);
+// Of codes: bf16 queries, up to 16 and 32 (heads of up to 128), float queries up to 16.
+int launch_attend_q8(const AttendArgs &a, hipStream_t s);
+int launch_attend_q8_32(const AttendArgs &a, hipStream_t s);
+int launch_attend_q8_f32(const AttendArgs &a, hipStream_t s);
 
 }  // namespace halo

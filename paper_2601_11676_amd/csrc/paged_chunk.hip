@@ -1,0 +1,92 @@
+// Attention of chunks of new tokens over a paged cache (halo_paged_chunk_attention, halo_paged_chunk_attention_q8): token i of a sequence, at position p_i, has
+//     o_h = sum_j p_j V_j,  p = softmax_j(scale q_h . K_j),  j <= p_i
+// one pass over the rows with the running maximum and sum of the softmax.  Products bound it: a cached row meets all the rows of a block, 32 or 128 queries (the heads of
+// one cache head, token by token).
+//
+// S^T = K Q^T      rows = tokens, columns = queries (matrix instruction of 32 x 32, 16 deep): a lane's results are scores of one query, so that maximum and sum
+//                  of a softmax need one exchange between the halves of a wave.
+// O^T += V^T P^T   the sum over tokens may take them in any order, so the operand P^T is what the lane already holds; V^T comes from LDS by the loads that
+//                  turn 4 x 16 elements on their way, four tokens of a dimension at a time.
+#include "paged_chunk.hpp"
+
+namespace halo {
+
+int check_paged_shape(const halo_paged_shape *s);
+int launch_chunk_bf16(const ChunkArgs &a, hipStream_t s) { return launch_chunk_dim<KindBf16>(a, s); }
+
+namespace {
+
+inline size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+constexpr int kMostSeqs = 4096, kMostTokens = 1 << 21;
+
+// What cut blocks leave: fewer than kParts blocks of a call are cut, into kParts parts and one more for each block.
+struct ChunkWorkspace {
+    size_t part = 0, bytes = 0;
+    ChunkWorkspace(const halo_paged_shape &s)
+    {
+        const size_t rows = (size_t)(2 * kParts) * 4 * kCol;
+        part = align256(rows * 2 * sizeof(float));
+        bytes = part + align256(rows * s.head_dim * sizeof(float));
+    }
+};
+
+int chunk(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, const float *k_scale, const void *v,
+          const float *v_scale, bool codes, int32_t n_seq, const int32_t *starts, const int32_t *table, const int32_t *lens, int32_t max_len,
+          const uint8_t *mask, float scale, void *out, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (const int rc = check_paged_shape(shape)) return rc;
+    if (N < 0 || N > kMostTokens || n_seq < 0 || n_seq > kMostSeqs) return HALO_ERR_ARG;
+    if (N == 0 || n_seq == 0) return HALO_OK;
+    if (!q || !k || !v || !starts || !table || !lens || !out || (codes && (!k_scale || !v_scale))) return HALO_ERR_NULL;
+    const halo_paged_shape &s = *shape;
+    const int size = s.dtype == HALO_F32 ? 4 : 2;
+    auto odd = [](const void *p, unsigned by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; };
+    if (max_len < 1 || max_len > s.max_pages * s.page_size || !std::isfinite(scale)) return HALO_ERR_ARG;
+    if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q, 16) || odd(k, 16) || odd(v, 16) || odd(out, 16) ||
+        odd(workspace, 16) || odd(k_scale, 4) || odd(v_scale, 4) || odd(starts, 4) || odd(table, 4) || odd(lens, 4))
+        return HALO_ERR_ARG;
+    const ChunkWorkspace ws(s);
+    if (!workspace || ws_bytes < ws.bytes) return HALO_ERR_WORKSPACE;
+
+    ChunkArgs a{};
+    a.q = q; a.k = k; a.v = v; a.k_scale = k_scale; a.v_scale = v_scale;
+    a.starts = starts; a.table = table; a.lens = lens; a.mask = mask; a.out = out;
+    a.stats = static_cast<float *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + ws.part);
+    a.q_stride = q_stride;
+    a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
+    a.N = N; a.n_seq = n_seq; a.n_heads = s.n_heads; a.group = s.n_heads / s.n_kv_heads; a.D = s.head_dim;
+    a.max_pages = s.max_pages; a.max_len = max_len;
+    a.scale2 = scale * 1.44269504088896341f;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (codes) return s.dtype == HALO_F32 ? launch_chunk_q8_f32(a, st) : launch_chunk_q8(a, st);
+    return s.dtype == HALO_F32 ? launch_chunk_f32(a, st) : launch_chunk_bf16(a, st);
+}
+
+}  // namespace
+}  // namespace halo
+
+extern "C" size_t halo_paged_chunk_workspace_bytes(const halo_paged_shape *shape, int32_t N, int32_t n_seq)
+{
+    using namespace halo;
+    if (check_paged_shape(shape) != HALO_OK || N < 0 || N > kMostTokens || n_seq < 0 || n_seq > kMostSeqs) return 0;
+    return ChunkWorkspace(*shape).bytes;
+}
+
+extern "C" int halo_paged_chunk_attention(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k_pages,
+                                          const void *v_pages, int32_t n_seq, const int32_t *starts, const int32_t *page_table,
+                                          const int32_t *lens, int32_t max_len, const uint8_t *mask, float scale, void *out, void *workspace,
+                                          size_t ws_bytes, void *stream)
+{
+    return halo::chunk(shape, N, q, q_stride, k_pages, nullptr, v_pages, nullptr, false, n_seq, starts, page_table, lens, max_len, mask, scale, out,
+                       workspace, ws_bytes, stream);
+}
+
+extern "C" int halo_paged_chunk_attention_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const int8_t *k_codes,
+                                             const float *k_scales, const int8_t *v_codes, const float *v_scales, int32_t n_seq,
+                                             const int32_t *starts, const int32_t *page_table, const int32_t *lens, int32_t max_len,
+                                             const uint8_t *mask, float scale, void *out, void *workspace, size_t ws_bytes, void *stream)
+{
+    return halo::chunk(shape, N, q, q_stride, k_codes, k_scales, v_codes, v_scales, true, n_seq, starts, page_table, lens, max_len, mask, scale, out,
+                       workspace, ws_bytes, stream);
+}
