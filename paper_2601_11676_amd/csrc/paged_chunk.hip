@@ -19,14 +19,13 @@ namespace {
 inline size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kMostSeqs = 4096, kMostTokens = 1 << 21;
 
-// What cut blocks leave: fewer than kParts blocks of a call are cut, into kParts parts and one more for each block.
+// What cut blocks leave.
 struct ChunkWorkspace {
     size_t part = 0, bytes = 0;
     ChunkWorkspace(const halo_paged_shape &s)
     {
-        const size_t rows = (size_t)(2 * kParts) * 4 * kCol;
-        part = align256(rows * 2 * sizeof(float));
-        bytes = part + align256(rows * s.head_dim * sizeof(float));
+        part = align256((size_t)kPartRows * 2 * sizeof(float));
+        bytes = part + align256((size_t)kPartRows * s.head_dim * sizeof(float));
     }
 };
 

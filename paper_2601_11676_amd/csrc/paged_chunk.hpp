@@ -29,9 +29,12 @@ struct ChunkArgs {
 namespace {
 
 constexpr int kCol = 32;                             // columns of the matrix instruction: rows of a block, that is queries
-constexpr int kParts = 512;                          // parts that few blocks are cut into, about
 constexpr int kLeast = 2;                            // tiles of a part at least
 constexpr int kDies = 8;
+// Parts that few blocks of so many rows are cut into, about: what is resident at once.
+constexpr int cuts(int rows) { return rows > kCol ? 256 : 512; }
+constexpr int kPartRows = 2 * 256 * 8 * kCol;        // rows of partial results: a part for each cut and one more for each block, fewer than cuts
+static_assert(2 * cuts(kCol) * kCol <= kPartRows, "of narrow blocks too");
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -64,6 +67,8 @@ struct KindQ8F32 {
     static constexpr bool kScaled = true, kCheckAll = false;
 };
 
+constexpr float kLargest = 0x1.fep127f;              // floats below it are finite as bf16
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -88,13 +93,16 @@ __device__ __forceinline__ void parts_of(const float (&x)[8], u32x4 (&out)[P])
     }
 }
 
-// Eight elements of the cache, as loaded; as bf16 parts.
-template <typename Cell> struct Eight;
-template <> struct Eight<bf16_t> {
+// 16 bytes of a row of the cache, as loaded, and as bf16 parts in LDS: words of two elements each.
+template <typename Cell> struct Piece;
+template <> struct Piece<bf16_t> {
+    static constexpr int kElems = 8, kWords = 4;
     u32x4 v;
-    __device__ __forceinline__ void load(const bf16_t *p) { v = *reinterpret_cast<const u32x4 *>(p); }
-    __device__ __forceinline__ void zero() { v = u32x4{0u, 0u, 0u, 0u}; }
-    __device__ __forceinline__ void parts(u32x4 (&out)[1]) const { out[0] = v; }
+    __device__ __forceinline__ void parts(uint32_t (&out)[1][4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[0][i] = v[i];
+    }
     // those that are no finite numbers become 0; whether there were any
     __device__ __forceinline__ bool mend()
     {
@@ -108,18 +116,21 @@ template <> struct Eight<bf16_t> {
         return any;
     }
 };
-template <> struct Eight<float> {
-    f32x4 a, b;
-    __device__ __forceinline__ void load(const float *p)
+template <> struct Piece<float> {
+    static constexpr int kElems = 4, kWords = 2;
+    u32x4 v;
+    __device__ __forceinline__ void parts(uint32_t (&out)[3][2]) const
     {
-        a = *reinterpret_cast<const f32x4 *>(p);
-        b = *reinterpret_cast<const f32x4 *>(p + 4);
-    }
-    __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
-    __device__ __forceinline__ void parts(u32x4 (&out)[3]) const
-    {
-        const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        parts_of<3>(x, out);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                out[p][i] = pack_bf16(a, b);
+                a -= bf16_lo(out[p][i]);
+                b -= bf16_hi(out[p][i]);
+            }
+        }
     }
     __device__ __forceinline__ bool mend()
     {
@@ -127,29 +138,36 @@ template <> struct Eight<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             // the largest floats, which round to infinity as bf16, count with the infinities: they are added as they are too
-            const bool x = !(fabsf(a[i]) < 0x1.fep127f), y = !(fabsf(b[i]) < 0x1.fep127f);
-            any = any || x || y;
-            a[i] = x ? 0.0f : a[i];
-            b[i] = y ? 0.0f : b[i];
+            const bool x = !(fabsf(__uint_as_float(v[i])) < kLargest);
+            any = any || x;
+            v[i] = x ? 0u : v[i];
         }
         return any;
     }
 };
-template <> struct Eight<int8_t> {
-    u32x2 v;
-    __device__ __forceinline__ void load(const int8_t *p) { v = *reinterpret_cast<const u32x2 *>(p); }
-    __device__ __forceinline__ void zero() { v = u32x2{0u, 0u}; }
-    __device__ __forceinline__ void parts(u32x4 (&out)[1]) const    // whole numbers up to 127 are bf16 numbers: a float's upper half
+template <> struct Piece<int8_t> {
+    static constexpr int kElems = 16, kWords = 8;
+    u32x4 v;
+    __device__ __forceinline__ void parts(uint32_t (&out)[1][8]) const    // whole numbers up to 127 are bf16 numbers: a float's upper half
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = v[i >> 1] >> (16 * (i & 1));
-            const float lo = (float)(int8_t)w, hi = (float)(int8_t)(w >> 8);
+        for (int i = 0; i < 8; ++i) {
+            const int w = (int)v[i >> 1];
+            const float lo = (float)(i & 1 ? (w << 8) >> 24 : (w << 24) >> 24), hi = (float)(i & 1 ? w >> 24 : (w << 16) >> 24);
             out[0][i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
         }
     }
     __device__ __forceinline__ bool mend() { return false; }
 };
+
+// Eight elements of a query as bf16 parts.
+__device__ __forceinline__ void query_parts(const bf16_t *p, u32x4 (&out)[1]) { out[0] = *reinterpret_cast<const u32x4 *>(p); }
+__device__ __forceinline__ void query_parts(const float *p, u32x4 (&out)[3])
+{
+    float x[8];
+    load8(p, x);
+    parts_of<3>(x, out);
+}
 
 // Wave-wide scans: a lane stands for a sequence.
 __device__ __forceinline__ int upto(int v, int lane)
@@ -202,7 +220,7 @@ struct Line {
                     all += (int64_t)s.blocks(a.group, kRows) * s.tiles(kTile);
                 }
             all = over_lanes(all) * a.pool.n_kv;
-            per = same((int)max((all + kParts - 1) / kParts, (int64_t)kLeast));
+            per = same((int)max((all + cuts(kRows) - 1) / cuts(kRows), (int64_t)kLeast));
         }
         for (int base = 0; base < a.n_seq; base += 64) {
             int mine = 0;
@@ -253,29 +271,41 @@ __device__ __forceinline__ void store_four(bf16_t *p, const float (&v)[4])
 }
 
 // A workgroup of WR * WK waves takes 32 WR rows of a cache head's queries; tiles of TT tokens, of which each of the WK waves of the same rows has
-// every WK-th 32.
+// every WK-th 32.  Two tiles in LDS, one being read while the next is written, where they have room beside another workgroup's.
 template <typename Kind, int DP, int WR, int WK>
 struct Layout {
+    typedef typename Kind::Cell Cell;
     static constexpr int kRows = WR * kCol, kWaves = WR * WK, kThreads = kWaves * 64;
-    static constexpr int TT = WK > 1 ? WK * 32 : DP * Kind::kC > 384 ? 32 : 64;
-    static constexpr int kUnits = DP / 8, kEach = TT * kUnits / kThreads;     // pieces of eight elements of a row; pieces of a thread
-    static constexpr int kPlane = TT * DP * 2, kTileBytes = Kind::kC * kPlane, kJoin = (WK - 1) * kRows * (DP + 2) * 4;
-    static constexpr int kLds = 2 * kTileBytes > kJoin ? 2 * kTileBytes : kJoin;
-    static_assert(TT * kUnits % kThreads == 0 && kThreads % kUnits == 0, "whole pieces");
+    static constexpr int TT = WK > 1 ? WK * 32 : DP * Kind::kC > 256 ? 32 : 64, kSub = TT / 32 / WK;
+    static constexpr int kPlane = TT * DP * 2, kTileBytes = 2 * Kind::kC * kPlane, kJoin = (WK - 1) * kRows * (DP + 2) * 4;
+    static constexpr int kBufs = kTileBytes <= 65536 ? 2 : 1;
+    static constexpr int kLds = kBufs * kTileBytes > kJoin ? kBufs * kTileBytes : kJoin;
+    // loads of a wave, 1 KiB each: of kRowsEach rows, which lie in one part of 16 tokens
+    static constexpr int kRowBytes = DP * (int)sizeof(Cell), kRowLanes = kRowBytes / 16, kRowsEach = 64 / kRowLanes, kLoads = TT / kRowsEach;
+    static constexpr int kEach = (kLoads + kWaves - 1) / kWaves, kParts16 = TT / 16;
+    static_assert(16 % kRowsEach == 0 && (kLoads % kWaves == 0 || kLoads < kWaves), "whole loads");
 };
 
+// Where a lane's 16 bytes lie in LDS: key rows are read 16 bytes a lane, a row a lane; value rows 16 dimensions of four rows at a time.  The pieces of a row change
+// places so that neither meets a bank twice.
+template <int DP> __device__ __forceinline__ int key_place(int row, int piece) { return row * DP * 2 + ((piece ^ (row & (DP < 128 ? 7 : 15))) << 4); }
+template <int DP> __device__ __forceinline__ int value_place(int row, int piece)
+{
+    const int f = ((row & 3) ^ ((row & 3) << 1)) << 1;
+    return row * DP * 2 + ((piece ^ (f & (DP / 8 - 1))) << 4);
+}
+
 template <typename Kind, int DP, bool EXACT, int WR, int WK>
-__global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
+__global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void chunk_attend(ChunkArgs a)
 {
     typedef Layout<Kind, DP, WR, WK> L;
     typedef typename Kind::Row Row;
     typedef typename Kind::Cell Cell;
-    constexpr int QS = DP / 16, DB = DP / 32, TT = L::TT;
+    typedef Piece<Cell> P;
+    constexpr int QS = DP / 16, DB = DP / 32, TT = L::TT, NS = L::kSub;
     __shared__ __align__(16) char s_tile[L::kLds];
-    __shared__ float s_scale[2][TT];
-    __shared__ int s_page[2][TT / 16];               // of the tile's parts of 16 tokens
-    __shared__ int s_bad;                            // values of the tile that are no finite numbers
-    char *const s_k = s_tile, *const s_v = s_tile + L::kTileBytes;
+    __shared__ __align__(16) float s_scale[L::kBufs][2][TT];
+    __shared__ int s_bad[L::kBufs];                  // values of the tile that are no finite numbers
     const int tid = threadIdx.x, lane = tid & 63, wave = same(tid >> 6), wr = wave / WK, wk = wave % WK;
     const int c = lane & 31, h = lane >> 5;
     const int D = EXACT ? DP : a.D;
@@ -285,7 +315,6 @@ __global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
     if (work < 0) return;
     const int kv = work / line.items;
     const int sq = line.find(a, work % line.items, lane);
-    const int *table = a.table + (int64_t)sq * a.max_pages;
     const int rows = line.seq.fresh * a.group, row0 = line.block * L::kRows, past = line.seq.len - line.seq.fresh;
 
     // the lane's row: a query head of a token, heads first
@@ -295,12 +324,32 @@ __global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
     const bool kept = !a.mask || a.mask[at * a.n_heads + head] != 0;
     const int lim = max(past + token + 1, 0);        // positions that it sees
     const int wave_last = min(row0 + (wr + 1) * kCol, rows) - 1, wave_first = min(row0 + wr * kCol, rows - 1);
-    const int most = max(past + wave_last / a.group + 1, 0), least = max(past + wave_first / a.group + 1, 0);
-    const int block_most = max(past + (min(row0 + L::kRows, rows) - 1) / a.group + 1, 0), block_least = max(past + row0 / a.group + 1, 0);
+    const int most = same(max(past + wave_last / a.group + 1, 0)), least = same(max(past + wave_first / a.group + 1, 0));
+    const int block_most = same(max(past + (min(row0 + L::kRows, rows) - 1) / a.group + 1, 0)), block_least = same(max(past + row0 / a.group + 1, 0));
     int tiles = (block_most + TT - 1) / TT;
     // a block without a row that counts reads nothing
-    if (!__syncthreads_or(kept && row < rows)) tiles = 0;
-    const int from = (int)((int64_t)tiles * line.part / line.parts), to = (int)((int64_t)tiles * (line.part + 1) / line.parts);
+    if (a.mask && !__syncthreads_or(kept && row < rows)) tiles = 0;
+    const int from = same((int)((int64_t)tiles * line.part / line.parts)), to = same((int)((int64_t)tiles * (line.part + 1) / line.parts));
+
+    // page numbers of the parts of 16 tokens, 64 parts at a time, a lane each
+    const int32_t *table = a.table + (int64_t)sq * a.max_pages;
+    int held = from * L::kParts16, id = 0, id_next = 0;
+    auto look = [&](int part) {
+        const int64_t pos = (int64_t)(part + lane) * 16;
+        int page = pos < block_most ? table[(int)pos >> a.pool.page_shift] : -1;
+        return page_exists(a.pool, page) ? page : -1;
+    };
+    if (from < to) id = look(held), id_next = look(held + 64);
+    auto page_of = [&](int part) {                   // wave-uniform, of the tile being computed or one of the two after it
+        const int n = part - held;
+        return n < 64 ? __builtin_amdgcn_readlane(id, n) : __builtin_amdgcn_readlane(id_next, n - 64);
+    };
+    auto advance = [&](int part) {                   // nobody asks for parts before this one any more
+        if (part - held < 64) return;
+        held += 64;
+        id = id_next;
+        id_next = look(held + 64);
+    };
 
     u32x4 qf[Kind::kQ][QS];
     {
@@ -309,9 +358,7 @@ __global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
         for (int s = 0; s < QS; ++s) {
             const int dim = s * 16 + h * 8;
             u32x4 p[Kind::kQ];
-            Eight<Row> e;
-            e.load(q + (EXACT || dim < D ? dim : 0));
-            e.parts(p);
+            query_parts(q + (EXACT || dim < D ? dim : 0), p);
 #pragma unroll
             for (int i = 0; i < Kind::kQ; ++i) qf[i][s] = EXACT || dim < D ? p[i] : u32x4{0u, 0u, 0u, 0u};
         }
@@ -323,110 +370,151 @@ __global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
 
-    // the thread's pieces of a tile on their way to LDS: those of row unit_row + i * kStep, columns unit * 8
-    constexpr int kStep = L::kThreads / L::kUnits;
-    const int unit = tid % L::kUnits, unit_row = tid / L::kUnits;
-    Eight<Cell> kp[L::kEach], vp[L::kEach];
+    // a tile's rows on their way to LDS: 16 bytes a lane and load
+    const int load_row = lane / L::kRowLanes, load_piece = lane % L::kRowLanes;
+    const uint32_t voff = EXACT || load_piece * P::kElems < D ? (uint32_t)(load_row * D * (int)sizeof(Cell) + load_piece * 16) : kOutOfRange;
+    P kp[L::kEach], vp[L::kEach];
     float kps = 0.0f, vps = 0.0f;
-    int page16 = 0;
     auto fetch = [&](int t) {
-        auto cell = [&](int r) {                     // row of the pools that holds position t * TT + r, or -1
-            const int pos = t * TT + r;
-            const int page = pos < block_most ? table[pos >> a.pool.page_shift] : -1;
-            return paged_row(a.pool, page, kv, pos);
-        };
 #pragma unroll
         for (int i = 0; i < L::kEach; ++i) {
-            const int64_t r = cell(unit_row + i * kStep);
-            if (r >= 0 && (EXACT || unit * 8 < D)) {
-                kp[i].load(static_cast<const Cell *>(a.k) + r * D + unit * 8);
-                vp[i].load(static_cast<const Cell *>(a.v) + r * D + unit * 8);
-            } else {
-                kp[i].zero();
-                vp[i].zero();
+            const int r = (wave + i * L::kWaves) * L::kRowsEach, pos = t * TT + r;
+            if (L::kLoads < L::kWaves && wave >= L::kLoads) break;
+            const int page = page_of(t * L::kParts16 + r / 16), live = page < 0 ? 0 : max(0, min(block_most - pos, L::kRowsEach));
+            const uint64_t row = (uint64_t)(page < 0 ? 0 : paged_row(a.pool, page, kv, pos)) * (uint64_t)(D * (int)sizeof(Cell));
+            const uint64_t byte = (uint64_t)(uint32_t)same((int)(row >> 32)) << 32 | (uint32_t)same((int)row);
+            const int bytes = same(live * D * (int)sizeof(Cell));
+            kp[i].v = buffer_load16<0>(buffer_of(static_cast<const char *>(a.k) + byte, bytes), voff, 0);
+            vp[i].v = buffer_load16<0>(buffer_of(static_cast<const char *>(a.v) + byte, bytes), voff, 0);
+        }
+        if constexpr (Kind::kScaled) {
+            if (tid < TT) {
+                const int pos = t * TT + tid, part = t * L::kParts16 + tid / 16 - held;
+                const int p0 = __shfl(id, part & 63), p1 = __shfl(id_next, part & 63);
+                const int page = part < 64 ? p0 : p1;
+                const bool in = page >= 0 && pos < block_most;
+                const int64_t r = in ? paged_row(a.pool, page, kv, pos) : 0;
+                kps = in ? a.k_scale[r] * a.scale2 : 0.0f;
+                vps = in ? a.v_scale[r] : 0.0f;
             }
         }
-        if (Kind::kScaled && tid < TT) {
-            const int64_t r = cell(tid);
-            kps = r >= 0 ? a.k_scale[r] : 0.0f;
-            vps = r >= 0 ? a.v_scale[r] : 0.0f;
-        }
-        if (tid < TT / 16) page16 = cell(tid * 16) >= 0;
     };
-    auto put = [&](int t) {
-        const bool check = Kind::kCheckAll || (t + 1) * TT > block_least;
-        bool bad = false;
+    auto put = [&](int t, int buf) {
+        char *const s_k = s_tile + buf * L::kTileBytes, *const s_v = s_k + L::kTileBytes / 2;
+        const bool check = Kind::kCheckAll || (!Kind::kScaled && (t + 1) * TT > block_least);
+        if (check) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < L::kEach; ++i) bad = vp[i].mend() || bad;
+            if (bad) s_bad[buf] = t + 1;
+        }
 #pragma unroll
         for (int i = 0; i < L::kEach; ++i) {
-            const int r = unit_row + i * kStep;
-            if (check) bad = vp[i].mend() || bad;
-            u32x4 p[Kind::kC];
-            kp[i].parts(p);
+            if (L::kLoads < L::kWaves && wave >= L::kLoads) break;
+            const int r = (wave + i * L::kWaves) * L::kRowsEach + load_row;
+            auto place = [&](const P &p, char *plane, bool value) {
+                uint32_t w[Kind::kC][P::kWords];
+                p.parts(w);
 #pragma unroll
-            for (int j = 0; j < Kind::kC; ++j)
-                *reinterpret_cast<u32x4 *>(s_k + j * L::kPlane + r * DP * 2 + ((unit ^ (r & (L::kUnits < 16 ? 7 : 15))) << 4)) = p[j];
-            vp[i].parts(p);
+                for (int j = 0; j < Kind::kC; ++j) {
+                    if constexpr (P::kWords == 2) {
+                        const int piece = load_piece >> 1;
+                        char *to = plane + j * L::kPlane + (value ? value_place<DP>(r, piece) : key_place<DP>(r, piece)) + (load_piece & 1) * 8;
+                        *reinterpret_cast<uint2 *>(to) = make_uint2(w[j][0], w[j][1]);
+                    } else {
 #pragma unroll
-            for (int j = 0; j < Kind::kC; ++j)
-                *reinterpret_cast<u32x4 *>(s_v + j * L::kPlane + r * DP * 2 + ((unit ^ ((r & 3) << 1)) << 4)) = p[j];
+                        for (int e = 0; e < P::kWords / 4; ++e) {
+                            const int piece = load_piece * (P::kWords / 4) + e;
+                            char *to = plane + j * L::kPlane + (value ? value_place<DP>(r, piece) : key_place<DP>(r, piece));
+                            *reinterpret_cast<u32x4 *>(to) = u32x4{w[j][4 * e], w[j][4 * e + 1], w[j][4 * e + 2], w[j][4 * e + 3]};
+                        }
+                    }
+                }
+            };
+            place(kp[i], s_k, false);
+            place(vp[i], s_v, true);
         }
-        if (Kind::kScaled && tid < TT) s_scale[0][tid] = kps, s_scale[1][tid] = vps;
-        if (tid < TT / 16) s_page[0][tid] = page16;
-        if (bad) s_bad = 1;
+        if (Kind::kScaled && tid < TT) s_scale[buf][0][tid] = kps, s_scale[buf][1][tid] = vps;
     };
 
-    // 32 tokens of a tile, from s0 on, against the wave's rows
-    auto step = [&](int t, int s0) {
-        const int pos0 = t * TT + s0;
-        f32x16 x;
+    // where the lane reads: 16 bytes of token c's key; four tokens' values of its dimension, as the loads that turn them want it
+    int key_at[QS], value_at[DB];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    for (int s = 0; s < QS; ++s) key_at[s] = key_place<DP>(c, s * 2 + h);
 #pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            if (!EXACT && s * 16 >= D) continue;
-            const int r = s0 + c, piece = s * 2 + h;
+    for (int d = 0; d < DB; ++d) {
+        const int dim = d * 32 + (lane & 16) + 4 * (lane & 3);
+        value_at[d] = value_place<DP>(4 * h + ((lane & 15) >> 2), dim >> 3) + (dim & 4) * 2;
+    }
+
+    // the wave's tokens of a tile against its rows
+    auto step = [&](int t, int buf) {
+        const char *const s_k = s_tile + buf * L::kTileBytes, *const s_v = s_k + L::kTileBytes / 2;
+        float x[NS][16], vs[NS][16];
 #pragma unroll
-            for (int j = 0; j < Kind::kC; ++j) {
-                const u32x4 kf = *reinterpret_cast<const u32x4 *>(s_k + j * L::kPlane + r * DP * 2 + ((piece ^ (r & (L::kUnits < 16 ? 7 : 15))) << 4));
+        for (int n = 0; n < NS; ++n) {
+            const int s0 = (n * WK + wk) * 32;
+            f32x16 sc;
 #pragma unroll
-                for (int i = 0; i < Kind::kQ; ++i)
-                    if (i + j < 3)
-                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[i][s]), x, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < QS; ++s) {
+                if (!EXACT && s * 16 >= D) continue;
+#pragma unroll
+                for (int j = 0; j < Kind::kC; ++j) {
+                    const u32x4 kf = *reinterpret_cast<const u32x4 *>(s_k + j * L::kPlane + s0 * DP * 2 + key_at[s]);
+#pragma unroll
+                    for (int i = 0; i < Kind::kQ; ++i)
+                        if (i + j < 3)
+                            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[i][s]), sc, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = sc[i];
+            if constexpr (Kind::kScaled) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const f32x4 ks = *reinterpret_cast<const f32x4 *>(&s_scale[buf][0][s0 + 8 * b + 4 * h]), w = *reinterpret_cast<const f32x4 *>(&s_scale[buf][1][s0 + 8 * b + 4 * h]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][4 * b + e] *= ks[e], vs[n][4 * b + e] = w[e];
+                }
             }
         }
-        float vs[16];
-        if constexpr (Kind::kScaled) {
+        // all seen by all rows, and scores whose order the scale keeps: the scale waits for the exponent
+        bool whole = (t + 1) * TT <= least, any = true;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const f32x4 ks = *reinterpret_cast<const f32x4 *>(&s_scale[0][s0 + 8 * b + 4 * h]), w = *reinterpret_cast<const f32x4 *>(&s_scale[1][s0 + 8 * b + 4 * h]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[4 * b + e] *= ks[e], vs[4 * b + e] = w[e];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= a.scale2;
-        bool any = true, whole = pos0 + 32 <= least;
-        const int p0 = s_page[0][s0 / 16], p1 = s_page[0][s0 / 16 + 1];
-        if (!(whole && p0 && p1)) {
+        for (int p = 0; p < L::kParts16; ++p) whole = whole && page_of(t * L::kParts16 + p) >= 0;
+        float by_scale = Kind::kScaled ? 1.0f : a.scale2;
+        if (!whole || !(by_scale > 0.0f)) {
             any = false;
-            whole = false;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 8 * (i / 4) + 4 * h + i % 4;
-                const bool sees = pos0 + r < lim && (i < 8 ? p0 : p1);
-                any = any || sees;
-                x[i] = sees ? x[i] : -INFINITY;
-                if (Kind::kScaled) vs[i] = sees ? vs[i] : 0.0f;
+            for (int n = 0; n < NS; ++n) {
+                const int s0 = (n * WK + wk) * 32, part = t * L::kParts16 + s0 / 16;
+                const bool p0 = page_of(part) >= 0, p1 = page_of(part + 1) >= 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 8 * (i / 4) + 4 * h + i % 4;
+                    const bool sees = t * TT + s0 + r < lim && (i < 8 ? p0 : p1);
+                    any = any || sees;
+                    x[n][i] = sees ? x[n][i] * by_scale : -INFINITY;
+                    if (Kind::kScaled) vs[n][i] = sees ? vs[n][i] : 0.0f;
+                }
             }
+            by_scale = 1.0f;
         }
-        float top = any ? -__FLT_MAX__ : -INFINITY;
+        float top = x[0][0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[n][i]);
         {
             const unsigned u = __builtin_bit_cast(unsigned, top);
             const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
             top = fmaxf(__builtin_bit_cast(float, (unsigned)both[0]), __builtin_bit_cast(float, (unsigned)both[1]));
         }
+        // positions that count lift the maximum to the lowest float at least: -infinity says that a row has none
+        if (!whole) any = __builtin_amdgcn_permlane32_swap((unsigned)any, (unsigned)any, false, false)[0] != 0 || __builtin_amdgcn_permlane32_swap((unsigned)any, (unsigned)any, false, false)[1] != 0;
+        top = fmaxf(top * by_scale, any ? -__FLT_MAX__ : -INFINITY);
         // The maximum only moves when a score passes it by 8 (a factor of 256, which float sums take with ease), so that most steps rescale nothing.
         const bool passed = top > m + 8.0f;
         if (__ballot(passed)) {
@@ -441,69 +529,93 @@ __global__ __launch_bounds__(WR * WK * 64) void chunk_attend(ChunkArgs a)
         }
         const float mm = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(x[i] - mm);
-        l += (((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]))) + (((x[8] + x[9]) + (x[10] + x[11])) + ((x[12] + x[13]) + (x[14] + x[15])));
-        if (Kind::kScaled)
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= vs[i];
+            for (int i = 0; i < 16; ++i) x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], by_scale, -mm));
+        if (Kind::kScaled || Kind::kP > 1) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            u32x4 pp[Kind::kP];
-            const float e[8] = {x[8 * ks], x[8 * ks + 1], x[8 * ks + 2], x[8 * ks + 3], x[8 * ks + 4], x[8 * ks + 5], x[8 * ks + 6], x[8 * ks + 7]};
-            parts_of<Kind::kP>(e, pp);
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                if (!EXACT && d * 32 >= D) continue;
-                const int r = s0 + 16 * ks + 4 * h + ((lane & 15) >> 2), dim = d * 32 + (lane & 16) + 4 * (lane & 3);
+                for (int i = 0; i < 16; i += 4) l += (x[n][i] + x[n][i + 1]) + (x[n][i + 2] + x[n][i + 3]);
+        }
+        if (Kind::kScaled) {
 #pragma unroll
-                for (int j = 0; j < Kind::kC; ++j) {
-                    auto turned = [&](int token) {
-                        typedef __attribute__((address_space(3))) s16x4 Lds;
-                        char *p = s_v + j * L::kPlane + token * DP * 2 + (((dim >> 3) ^ ((token & 3) << 1)) << 4) + (dim & 4) * 2;
-                        return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)p));
-                    };
-                    const u32x2 lo = turned(r), hi = turned(r + 8);
-                    const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
+            for (int n = 0; n < NS; ++n)
 #pragma unroll
-                    for (int i = 0; i < Kind::kP; ++i)
-                        if (i + j < 3)
-                            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pp[i]), acc[d], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) x[n][i] *= vs[n][i];
+        }
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int s0 = (n * WK + wk) * 32;
+                u32x4 pp[Kind::kP];
+                const float e[8] = {x[n][8 * ks], x[n][8 * ks + 1], x[n][8 * ks + 2], x[n][8 * ks + 3], x[n][8 * ks + 4], x[n][8 * ks + 5], x[n][8 * ks + 6], x[n][8 * ks + 7]};
+                parts_of<Kind::kP>(e, pp);
+                if (!Kind::kScaled && Kind::kP == 1) {       // the sum is of what is multiplied: the weights add up to one
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l = dot2_bf16(pp[0][i], 0x3f803f80u, l);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    if (!EXACT && d * 32 >= D) continue;
+#pragma unroll
+                    for (int j = 0; j < Kind::kC; ++j) {
+                        auto turned = [&](int token) {
+                            typedef __attribute__((address_space(3))) s16x4 Lds;
+                            return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)(s_v + j * L::kPlane + token * DP * 2 + value_at[d])));
+                        };
+                        const u32x2 lo = turned(s0 + 16 * ks), hi = turned(s0 + 16 * ks + 8);
+                        const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+                        for (int i = 0; i < Kind::kP; ++i)
+                            if (i + j < 3)
+                                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pp[i]), acc[d], 0, 0, 0);
+                    }
                 }
             }
-        }
         // Values that are no finite numbers were left out of the products (0 * infinity would reach the rows that do not see them): they are added as they
         // are to the rows that do.
         if constexpr (!Kind::kScaled) {
-            if (s_bad)
-                for (int tt = 0; tt < 32; ++tt) {
-                    const int pos = pos0 + tt, page = pos < block_most ? table[pos >> a.pool.page_shift] : -1;
-                    const int64_t r = paged_row(a.pool, page, kv, pos);
-                    if (r < 0) continue;
-                    const Cell *v = static_cast<const Cell *>(a.v) + r * D;
+            if (s_bad[buf] == t + 1)
+                for (int tt = 0; tt < 32 * NS; ++tt) {
+                    const int r0 = (tt / 32 * WK + wk) * 32 + tt % 32, pos = t * TT + r0, page = page_of(t * L::kParts16 + r0 / 16);
+                    if (page < 0 || pos >= block_most) continue;
+                    const Cell *v = static_cast<const Cell *>(a.v) + paged_row(a.pool, page, kv, pos) * D;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int dim = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
                             const float w = EXACT || dim < D ? to_float(v[dim]) : 0.0f;
-                            if (!(fabsf(w) < (Kind::kC > 1 ? 0x1.fep127f : INFINITY)) && pos < lim) acc[d][i] += w;
+                            if (!(fabsf(w) < (Kind::kC > 1 ? kLargest : INFINITY)) && pos < lim) acc[d][i] += w;
                         }
                 }
         }
     };
 
-    if (tid == 0) s_bad = 0;
+    if (tid < L::kBufs) s_bad[tid] = 0;
     if (from < to) fetch(from);
-    for (int t = from; t < to; ++t) {
-        __syncthreads();
-        if (tid == 0) s_bad = 0;
-        __syncthreads();
-        put(t);
-        if (t + 1 < to) fetch(t + 1);
-        __syncthreads();
-#pragma unroll 1
-        for (int s0 = wk * 32; s0 < TT; s0 += WK * 32)
-            if (t * TT + s0 < most) step(t, s0);
+    __syncthreads();
+    if constexpr (L::kBufs == 2) {
+        if (from < to) put(from, 0);
+        for (int t = from; t < to; ++t) {
+            const int buf = (t - from) & 1;
+            __syncthreads();
+            advance(t * L::kParts16);
+            if (t + 1 < to) fetch(t + 1);
+            if (t * TT < most) step(t, buf);
+            if (t + 1 < to) put(t + 1, buf ^ 1);
+        }
+    } else {
+        for (int t = from; t < to; ++t) {
+            put(t, 0);
+            __syncthreads();
+            advance(t * L::kParts16);
+            if (t + 1 < to) fetch(t + 1);
+            if (t * TT < most) step(t, 0);
+            __syncthreads();
+        }
     }
     l = xor_add<32>(l);
 
@@ -616,9 +728,9 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     typedef Layout<Kind, DP, WR, WK> L;
     const int64_t blocks = most_blocks(a, L::kRows);
     int64_t grid = blocks;
-    const bool cut = blocks < kParts && a.max_len > kLeast * L::TT;
+    const bool cut = blocks < cuts(L::kRows) && a.max_len > kLeast * L::TT;
     if (cut) {
-        grid += kParts;                              // a part more than even shares give, for each block
+        grid += cuts(L::kRows);                              // a part more than even shares give, for each block
         a.slots = (int)grid;
     }
     a.most = (int)grid;
@@ -633,9 +745,13 @@ int launch_rows(ChunkArgs a, hipStream_t s)
 template <typename Kind, int DP, bool EXACT>
 int launch_chunk(const ChunkArgs &a, hipStream_t s)
 {
+#ifndef WIDE
+#define WIDE 8
+#endif
+    constexpr int kWide = DP * Kind::kC > 128 ? 4 : WIDE;
     constexpr int kNarrow = DP * Kind::kC > 512 ? 1 : DP * Kind::kC > 256 ? 2 : 4;      // waves of the same rows that LDS has room for
     if ((int64_t)a.N * a.group <= (int64_t)kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 1, kNarrow>(a, s);
-    return launch_rows<Kind, DP, EXACT, 4, 1>(a, s);
+    return launch_rows<Kind, DP, EXACT, kWide, 1>(a, s);
 }
 
 template <typename Kind>
