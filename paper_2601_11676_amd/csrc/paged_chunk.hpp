@@ -9,6 +9,9 @@
 #include "kernels.hpp"
 #include "paged_index.hpp"
 
+#ifndef AHEAD
+#define AHEAD 4
+#endif
 namespace halo {
 
 struct ChunkArgs {
@@ -32,7 +35,7 @@ constexpr int kCol = 32;                             // columns of the matrix in
 constexpr int kLeast = 2;                            // tiles of a part at least
 constexpr int kDies = 8;
 // Parts that few blocks of so many rows are cut into, about: what is resident at once.
-constexpr int cuts(int rows) { return rows > kCol ? 256 : 512; }
+constexpr int cuts(int rows) { return rows >= 256 ? 256 : 512; }
 constexpr int kPartRows = 2 * 256 * 8 * kCol;        // rows of partial results: a part for each cut and one more for each block, fewer than cuts
 static_assert(2 * cuts(kCol) * kCol <= kPartRows, "of narrow blocks too");
 
@@ -203,64 +206,100 @@ __device__ __forceinline__ Sequence sequence(const ChunkArgs &a, int s)
     return r;
 }
 
-// The line of all parts of all blocks of rows of one cache head, sequence by sequence, the blocks that see the most first.
+// The line of all parts of all blocks of rows of one cache head: sequence by sequence, long ones first (up to 64 of them; of more in their order), and a sequence's blocks that see
+// the most first, so that what begins last is short.  All of a wave-uniform; a lane has a sequence.
 template <int kRows, int kTile>
 struct Line {
     int per, items;                                  // tiles of a part at most (0: nothing is cut); parts of a cache head
-    Sequence seq;                                    // what find() found
+    Sequence own;                                    // up to 64 sequences: of the lane's, in the line's order; its number and the parts up to its end
+    int number, end;
+    Sequence seq;                                    // what find() found: sequence, block of rows, part of so many
     int block, part, parts;
 
-    __device__ __forceinline__ Line(const ChunkArgs &a, int lane) : per(0), items(0)
+    __device__ __forceinline__ Line(const ChunkArgs &a, int lane) : per(0), items(0), number(lane), end(0)
     {
+        const bool few = a.n_seq <= 64;
+        if (few) {
+            own = sequence(a, min(lane, a.n_seq - 1));
+            if (lane >= a.n_seq) own.fresh = 0, own.len = 0;
+            int rank = 0;
+            for (int i = 0; i < a.n_seq; ++i) {
+                const int other = __builtin_amdgcn_readlane(own.len, i);
+                rank += other > own.len || (other == own.len && i < lane);
+            }
+            const int to = (lane < a.n_seq ? rank : lane) * 4;
+            number = __builtin_amdgcn_ds_permute(to, lane);
+            own.first = __builtin_amdgcn_ds_permute(to, own.first);
+            own.fresh = __builtin_amdgcn_ds_permute(to, own.fresh);
+            own.len = __builtin_amdgcn_ds_permute(to, own.len);
+        }
         if (a.slots > 0) {
             int64_t all = 0;
-            for (int base = 0; base < a.n_seq; base += 64)
-                if (base + lane < a.n_seq) {
-                    const Sequence s = sequence(a, base + lane);
+            if (few) {
+                all = (int64_t)own.blocks(a.group, kRows) * own.tiles(kTile);
+            } else {
+                for (int i = lane; i < a.n_seq; i += 64) {
+                    const Sequence s = sequence(a, i);
                     all += (int64_t)s.blocks(a.group, kRows) * s.tiles(kTile);
                 }
+            }
             all = over_lanes(all) * a.pool.n_kv;
             per = same((int)max((all + cuts(kRows) - 1) / cuts(kRows), (int64_t)kLeast));
         }
-        for (int base = 0; base < a.n_seq; base += 64) {
-            int mine = 0;
-            if (base + lane < a.n_seq) {
-                const Sequence s = sequence(a, base + lane);
-                mine = s.blocks(a.group, kRows) * s.parts(kTile, per);
+        if (few) {
+            end = upto(own.blocks(a.group, kRows) * own.parts(kTile, per), lane);
+            items = __builtin_amdgcn_readlane(end, 63);
+        } else {
+            for (int base = 0; base < a.n_seq; base += 64) {
+                int mine = 0;
+                if (base + lane < a.n_seq) {
+                    const Sequence s = sequence(a, base + lane);
+                    mine = s.blocks(a.group, kRows) * s.parts(kTile, per);
+                }
+                items = min(items + __builtin_amdgcn_readlane(upto(mine, lane), 63), a.most);
             }
-            items = min(items + __builtin_amdgcn_readlane(upto(mine, lane), 63), a.most);
         }
+        items = min(items, a.most);
     }
-    // the n-th, n < items; all wave-uniform.  Returns its sequence's number.
+    __device__ __forceinline__ int take(const ChunkArgs &a, const Sequence &s, int mine, int upto_end, int name, int n, int at)
+    {
+        n -= __builtin_amdgcn_readlane(upto_end - mine, at);
+        seq.first = __builtin_amdgcn_readlane(s.first, at);
+        seq.fresh = __builtin_amdgcn_readlane(s.fresh, at);
+        seq.len = __builtin_amdgcn_readlane(s.len, at);
+        parts = seq.parts(kTile, per);
+        const int blocks = seq.blocks(a.group, kRows);
+        block = max(blocks - 1 - n / parts, 0);
+        part = n % parts;
+        return __builtin_amdgcn_readlane(name, at);
+    }
+    // the n-th, n < items.  Returns its sequence's number.
     __device__ __forceinline__ int find(const ChunkArgs &a, int n, int lane)
     {
+        if (a.n_seq <= 64) return take(a, own, own.blocks(a.group, kRows) * own.parts(kTile, per), end, number, n, min((int)__popcll(__ballot(end <= n)), 63));
         for (int base = 0;; base += 64) {
             int mine = 0;
             const Sequence s = sequence(a, min(base + lane, a.n_seq - 1));
             if (base + lane < a.n_seq) mine = s.blocks(a.group, kRows) * s.parts(kTile, per);
-            const int end = upto(mine, lane), all = __builtin_amdgcn_readlane(end, 63);
+            const int last = upto(mine, lane), all = __builtin_amdgcn_readlane(last, 63);
             if (n >= all && base + 64 < a.n_seq) {
                 n -= all;
                 continue;
             }
-            const int at = min((int)__popcll(__ballot(end <= n)), 63);
-            n -= __builtin_amdgcn_readlane(end - mine, at);
-            seq.first = __builtin_amdgcn_readlane(s.first, at);
-            seq.fresh = __builtin_amdgcn_readlane(s.fresh, at);
-            seq.len = __builtin_amdgcn_readlane(s.len, at);
-            parts = seq.parts(kTile, per);
-            block = max(seq.blocks(a.group, kRows) - 1 - n / parts, 0);
-            part = n % parts;
-            return base + at;
+            return take(a, s, mine, last, base + lane, n, min((int)__popcll(__ballot(last <= n)), 63));
         }
     }
 };
 
-// The place of a workgroup in a line of `all`: a die takes neighbours, which read the same rows.  -1: none.
-__device__ __forceinline__ int place_of(int block, int all)
+// A workgroup's part of the line and cache head: neighbours of the line, all heads of one after those of the other.  Workgroup i runs on die i % 8: where the cache heads are
+// a multiple of the dies, each die has heads of its own, whose rows its L2 then serves to all that read them.
+__device__ __forceinline__ bool place_of(const ChunkArgs &a, int block, int items, int &item, int &kv)
 {
-    const int per = (all + kDies - 1) / kDies, slot = block / kDies, at = block % kDies * per + slot;
-    return slot < per && at < all ? at : -1;
+    const int heads = a.pool.n_kv % kDies == 0 ? a.pool.n_kv / kDies : a.pool.n_kv;
+    const int slot = heads < a.pool.n_kv ? block / kDies : block;
+    item = slot / heads;
+    kv = slot - item * heads + (heads < a.pool.n_kv ? block % kDies * heads : 0);
+    return item < items && (int64_t)item * a.pool.n_kv + kv < a.most;
 }
 
 __device__ __forceinline__ void store_four(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
@@ -278,11 +317,11 @@ struct Layout {
     static constexpr int kRows = WR * kCol, kWaves = WR * WK, kThreads = kWaves * 64;
     static constexpr int TT = WK > 1 ? WK * 32 : DP * Kind::kC > 256 ? 32 : 64, kSub = TT / 32 / WK;
     static constexpr int kPlane = TT * DP * 2, kTileBytes = 2 * Kind::kC * kPlane, kJoin = (WK - 1) * kRows * (DP + 2) * 4;
-    static constexpr int kBufs = kTileBytes <= 65536 ? 2 : 1;
+    static constexpr int kBufs = kTileBytes <= 65536 ? 2 : 1, kRowsBytes = kTileBytes / 2;
     static constexpr int kLds = kBufs * kTileBytes > kJoin ? kBufs * kTileBytes : kJoin;
     // loads of a wave, 1 KiB each: of kRowsEach rows, which lie in one part of 16 tokens
     static constexpr int kRowBytes = DP * (int)sizeof(Cell), kRowLanes = kRowBytes / 16, kRowsEach = 64 / kRowLanes, kLoads = TT / kRowsEach;
-    static constexpr int kEach = (kLoads + kWaves - 1) / kWaves, kParts16 = TT / 16;
+    static constexpr int kEach = (kLoads + kWaves - 1) / kWaves, kParts16 = TT / 16, kPerPart = kEach * kRowsEach > 16 ? 16 / kRowsEach : kEach;
     static_assert(16 % kRowsEach == 0 && (kLoads % kWaves == 0 || kLoads < kWaves), "whole loads");
 };
 
@@ -295,6 +334,24 @@ template <int DP> __device__ __forceinline__ int value_place(int row, int piece)
     return row * DP * 2 + ((piece ^ (f & (DP / 8 - 1))) << 4);
 }
 
+// Products of parts that are taken.
+constexpr int products(int a, int b) { return a * b < 9 ? a * b : 6; }
+
+// The order of a run of matrix instructions and of the loads from LDS of their operands, READS loads an operand: AHEAD operands first, then one for each that is used up
+// (left to itself the compiler loads one ahead and waits out the latency at every second instruction).
+template <int OPERANDS, int MFMAS, int READS>
+__device__ __forceinline__ void reads_ahead()
+{
+    constexpr int kAhead = AHEAD < OPERANDS ? AHEAD : OPERANDS;
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead * READS, 0);
+#pragma unroll
+    for (int i = 0; i < OPERANDS - kAhead; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kAhead * MFMAS, 0);
+}
+
 template <typename Kind, int DP, bool EXACT, int WR, int WK>
 __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void chunk_attend(ChunkArgs a)
 {
@@ -305,16 +362,15 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     constexpr int QS = DP / 16, DB = DP / 32, TT = L::TT, NS = L::kSub;
     __shared__ __align__(16) char s_tile[L::kLds];
     __shared__ __align__(16) float s_scale[L::kBufs][2][TT];
-    __shared__ int s_bad[L::kBufs];                  // values of the tile that are no finite numbers
+    __shared__ int s_bad[L::kBufs];                  // 1 + the tile whose values have some that are no finite numbers
     const int tid = threadIdx.x, lane = tid & 63, wave = same(tid >> 6), wr = wave / WK, wk = wave % WK;
     const int c = lane & 31, h = lane >> 5;
     const int D = EXACT ? DP : a.D;
 
     Line<L::kRows, TT> line(a, lane);
-    const int work = place_of(blockIdx.x, (int)min((int64_t)line.items * a.pool.n_kv, (int64_t)a.most));
-    if (work < 0) return;
-    const int kv = work / line.items;
-    const int sq = line.find(a, work % line.items, lane);
+    int item, kv;
+    if (!place_of(a, blockIdx.x, line.items, item, kv)) return;
+    const int sq = line.find(a, item, lane);
     const int rows = line.seq.fresh * a.group, row0 = line.block * L::kRows, past = line.seq.len - line.seq.fresh;
 
     // the lane's row: a query head of a token, heads first
@@ -324,31 +380,44 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     const bool kept = !a.mask || a.mask[at * a.n_heads + head] != 0;
     const int lim = max(past + token + 1, 0);        // positions that it sees
     const int wave_last = min(row0 + (wr + 1) * kCol, rows) - 1, wave_first = min(row0 + wr * kCol, rows - 1);
-    const int most = same(max(past + wave_last / a.group + 1, 0)), least = same(max(past + wave_first / a.group + 1, 0));
+    const int most = row0 + wr * kCol < rows ? same(max(past + wave_last / a.group + 1, 0)) : 0,      // a wave without rows reads nothing
+         least = same(max(past + wave_first / a.group + 1, 0));
     const int block_most = same(max(past + (min(row0 + L::kRows, rows) - 1) / a.group + 1, 0)), block_least = same(max(past + row0 / a.group + 1, 0));
     int tiles = (block_most + TT - 1) / TT;
     // a block without a row that counts reads nothing
     if (a.mask && !__syncthreads_or(kept && row < rows)) tiles = 0;
     const int from = same((int)((int64_t)tiles * line.part / line.parts)), to = same((int)((int64_t)tiles * (line.part + 1) / line.parts));
 
-    // page numbers of the parts of 16 tokens, 64 parts at a time, a lane each
+    // page numbers of the parts of 16 tokens, 64 parts at a time, a lane each (-1: no page), and which are pages
     const int32_t *table = a.table + (int64_t)sq * a.max_pages;
     int held = from * L::kParts16, id = 0, id_next = 0;
+    uint64_t pages = 0, pages_next = 0;
     auto look = [&](int part) {
         const int64_t pos = (int64_t)(part + lane) * 16;
         int page = pos < block_most ? table[(int)pos >> a.pool.page_shift] : -1;
         return page_exists(a.pool, page) ? page : -1;
     };
-    if (from < to) id = look(held), id_next = look(held + 64);
-    auto page_of = [&](int part) {                   // wave-uniform, of the tile being computed or one of the two after it
-        const int n = part - held;
-        return n < 64 ? __builtin_amdgcn_readlane(id, n) : __builtin_amdgcn_readlane(id_next, n - 64);
+    if (from < to) {
+        id = look(held), id_next = look(held + 64);
+        pages = __ballot(id >= 0), pages_next = __ballot(id_next >= 0);
+    }
+    // both wave-uniform, of the tile being computed, one before or two after it: a part's page; whether all parts of a tile are pages
+    auto page_of = [&](int part) {
+        const int n = part - held, p0 = __builtin_amdgcn_readlane(id, n & 63), p1 = __builtin_amdgcn_readlane(id_next, n & 63);
+        return n < 64 ? p0 : p1;
+    };
+    auto all_pages = [&](int t) {                    // 64 is a multiple of a tile's parts
+        constexpr uint64_t kAll = (1ull << L::kParts16) - 1;
+        const int n = t * L::kParts16 - held;
+        return (((n < 64 ? pages : pages_next) >> (n & 63)) & kAll) == kAll;
     };
     auto advance = [&](int part) {                   // nobody asks for parts before this one any more
         if (part - held < 64) return;
         held += 64;
         id = id_next;
+        pages = pages_next;
         id_next = look(held + 64);
+        pages_next = __ballot(id_next >= 0);
     };
 
     u32x4 qf[Kind::kQ][QS];
@@ -375,46 +444,44 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     const uint32_t voff = EXACT || load_piece * P::kElems < D ? (uint32_t)(load_row * D * (int)sizeof(Cell) + load_piece * 16) : kOutOfRange;
     P kp[L::kEach], vp[L::kEach];
     float kps = 0.0f, vps = 0.0f;
+    // Without a condition: rows that are none, and tiles past the last, are descriptors of no bytes (a load that may not be made would have its registers copied, and that
+    // waits for it).
     auto fetch = [&](int t) {
+        constexpr int kRow = (int)sizeof(Cell);
 #pragma unroll
-        for (int i = 0; i < L::kEach; ++i) {
-            const int r = (wave + i * L::kWaves) * L::kRowsEach, pos = t * TT + r;
-            if (L::kLoads < L::kWaves && wave >= L::kLoads) break;
-            const int page = page_of(t * L::kParts16 + r / 16), live = page < 0 ? 0 : max(0, min(block_most - pos, L::kRowsEach));
-            const uint64_t row = (uint64_t)(page < 0 ? 0 : paged_row(a.pool, page, kv, pos)) * (uint64_t)(D * (int)sizeof(Cell));
+        for (int j = 0; j < L::kEach; j += L::kPerPart) {
+            const int r = (wave * L::kEach + j) % L::kLoads * L::kRowsEach, pos = t * TT + r;
+            const int page = page_of(t * L::kParts16 + r / 16);
+            const int live = page < 0 || t >= to ? 0 : max(0, min(block_most - pos, L::kPerPart * L::kRowsEach));
+            const uint64_t row = ((((uint64_t)max(page, 0) * a.pool.n_kv + kv) << a.pool.page_shift) + (pos & ((1 << a.pool.page_shift) - 1))) * (uint64_t)(D * kRow);
             const uint64_t byte = (uint64_t)(uint32_t)same((int)(row >> 32)) << 32 | (uint32_t)same((int)row);
-            const int bytes = same(live * D * (int)sizeof(Cell));
-            kp[i].v = buffer_load16<0>(buffer_of(static_cast<const char *>(a.k) + byte, bytes), voff, 0);
-            vp[i].v = buffer_load16<0>(buffer_of(static_cast<const char *>(a.v) + byte, bytes), voff, 0);
+            const int bytes = same(live * D * kRow);
+            const auto k_rows = buffer_of(static_cast<const char *>(a.k) + byte, bytes), v_rows = buffer_of(static_cast<const char *>(a.v) + byte, bytes);
+#pragma unroll
+            for (int i = 0; i < L::kPerPart; ++i) kp[j + i].v = buffer_load16<0>(k_rows, voff + i * L::kRowsEach * D * kRow, 0);
+#pragma unroll
+            for (int i = 0; i < L::kPerPart; ++i) vp[j + i].v = buffer_load16<0>(v_rows, voff + i * L::kRowsEach * D * kRow, 0);
         }
         if constexpr (Kind::kScaled) {
             if (tid < TT) {
                 const int pos = t * TT + tid, part = t * L::kParts16 + tid / 16 - held;
                 const int p0 = __shfl(id, part & 63), p1 = __shfl(id_next, part & 63);
                 const int page = part < 64 ? p0 : p1;
-                const bool in = page >= 0 && pos < block_most;
+                const bool in = page >= 0 && pos < block_most && t < to;
                 const int64_t r = in ? paged_row(a.pool, page, kv, pos) : 0;
                 kps = in ? a.k_scale[r] * a.scale2 : 0.0f;
                 vps = in ? a.v_scale[r] : 0.0f;
             }
         }
     };
-    auto put = [&](int t, int buf) {
-        char *const s_k = s_tile + buf * L::kTileBytes, *const s_v = s_k + L::kTileBytes / 2;
-        const bool check = Kind::kCheckAll || (!Kind::kScaled && (t + 1) * TT > block_least);
-        if (check) {
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < L::kEach; ++i) bad = vp[i].mend() || bad;
-            if (bad) s_bad[buf] = t + 1;
-        }
+    auto put_rows = [&](const P (&from)[L::kEach], char *plane, bool value) {
 #pragma unroll
         for (int i = 0; i < L::kEach; ++i) {
             if (L::kLoads < L::kWaves && wave >= L::kLoads) break;
-            const int r = (wave + i * L::kWaves) * L::kRowsEach + load_row;
-            auto place = [&](const P &p, char *plane, bool value) {
+            const int r = (wave * L::kEach + i) * L::kRowsEach + load_row;
+            {
                 uint32_t w[Kind::kC][P::kWords];
-                p.parts(w);
+                from[i].parts(w);
 #pragma unroll
                 for (int j = 0; j < Kind::kC; ++j) {
                     if constexpr (P::kWords == 2) {
@@ -430,11 +497,21 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
                         }
                     }
                 }
-            };
-            place(kp[i], s_k, false);
-            place(vp[i], s_v, true);
+            }
         }
+    };
+    auto keys_of = [&](int buf) { return s_tile + buf * L::kRowsBytes; };
+    auto values_of = [&](int buf) { return s_tile + (L::kBufs + buf) * L::kRowsBytes; };
+    auto put = [&](int t, int buf) {
+        put_rows(kp, keys_of(buf), false);
         if (Kind::kScaled && tid < TT) s_scale[buf][0][tid] = kps, s_scale[buf][1][tid] = vps;
+        if (Kind::kCheckAll || (!Kind::kScaled && (t + 1) * TT > block_least)) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < L::kEach; ++i) bad = vp[i].mend() || bad;
+            if (bad) s_bad[buf] = t + 1;
+        }
+        put_rows(vp, values_of(buf), true);
     };
 
     // where the lane reads: 16 bytes of token c's key; four tokens' values of its dimension, as the loads that turn them want it
@@ -447,31 +524,42 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
         value_at[d] = value_place<DP>(4 * h + ((lane & 15) >> 2), dim >> 3) + (dim & 4) * 2;
     }
 
-    // the wave's tokens of a tile against its rows
-    auto step = [&](int t, int buf) {
-        const char *const s_k = s_tile + buf * L::kTileBytes, *const s_v = s_k + L::kTileBytes / 2;
-        float x[NS][16], vs[NS][16];
+    // the wave's tokens of a tile against its rows: scores, probabilities, products with the values
+    float x[NS][16];
+    u32x4 pp[NS][2][Kind::kP];
+    auto scores = [&](int t, int buf) {
+        const char *const s_k = keys_of(buf);
+        f32x16 sc[NS];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            const int s0 = (n * WK + wk) * 32;
-            f32x16 sc;
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+            for (int i = 0; i < 16; ++i) sc[n][i] = 0.0f;
 #pragma unroll
-            for (int s = 0; s < QS; ++s) {
-                if (!EXACT && s * 16 >= D) continue;
+        for (int s = 0; s < QS; ++s) {
+            if (!EXACT && s * 16 >= D) continue;
 #pragma unroll
-                for (int j = 0; j < Kind::kC; ++j) {
-                    const u32x4 kf = *reinterpret_cast<const u32x4 *>(s_k + j * L::kPlane + s0 * DP * 2 + key_at[s]);
+            for (int j = 0; j < Kind::kC; ++j)
+#pragma unroll
+                for (int n = 0; n < NS; ++n) {
+                    const u32x4 kf = *reinterpret_cast<const u32x4 *>(s_k + j * L::kPlane + (n * WK + wk) * 32 * DP * 2 + key_at[s]);
 #pragma unroll
                     for (int i = 0; i < Kind::kQ; ++i)
                         if (i + j < 3)
-                            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[i][s]), sc, 0, 0, 0);
+                            sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[i][s]), sc[n], 0, 0, 0);
                 }
-            }
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[n][i] = sc[i];
-            if constexpr (Kind::kScaled) {
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[n][i] = sc[n][i];
+        if constexpr (EXACT) reads_ahead<NS * QS * Kind::kC, products(Kind::kQ, Kind::kC) / Kind::kC, 1>();
+    };
+    auto soften = [&](int t, int buf) {
+        float vs[NS][16];
+        if constexpr (Kind::kScaled) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const int s0 = (n * WK + wk) * 32;
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const f32x4 ks = *reinterpret_cast<const f32x4 *>(&s_scale[buf][0][s0 + 8 * b + 4 * h]), w = *reinterpret_cast<const f32x4 *>(&s_scale[buf][1][s0 + 8 * b + 4 * h]);
@@ -481,9 +569,7 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
             }
         }
         // all seen by all rows, and scores whose order the scale keeps: the scale waits for the exponent
-        bool whole = (t + 1) * TT <= least, any = true;
-#pragma unroll
-        for (int p = 0; p < L::kParts16; ++p) whole = whole && page_of(t * L::kParts16 + p) >= 0;
+        bool whole = (t + 1) * TT <= least && all_pages(t), any = true;
         float by_scale = Kind::kScaled ? 1.0f : a.scale2;
         if (!whole || !(by_scale > 0.0f)) {
             any = false;
@@ -548,14 +634,21 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
         for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                const int s0 = (n * WK + wk) * 32;
-                u32x4 pp[Kind::kP];
                 const float e[8] = {x[n][8 * ks], x[n][8 * ks + 1], x[n][8 * ks + 2], x[n][8 * ks + 3], x[n][8 * ks + 4], x[n][8 * ks + 5], x[n][8 * ks + 6], x[n][8 * ks + 7]};
-                parts_of<Kind::kP>(e, pp);
+                parts_of<Kind::kP>(e, pp[n][ks]);
                 if (!Kind::kScaled && Kind::kP == 1) {       // the sum is of what is multiplied: the weights add up to one
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) l = dot2_bf16(pp[0][i], 0x3f803f80u, l);
+                    for (int i = 0; i < 4; ++i) l = dot2_bf16(pp[n][ks][0][i], 0x3f803f80u, l);
                 }
+            }
+    };
+    auto product = [&](int t, int buf) {
+        const char *const s_v = values_of(buf);
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int s0 = (n * WK + wk) * 32;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     if (!EXACT && d * 32 >= D) continue;
@@ -570,10 +663,11 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
 #pragma unroll
                         for (int i = 0; i < Kind::kP; ++i)
                             if (i + j < 3)
-                                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pp[i]), acc[d], 0, 0, 0);
+                                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf), __builtin_bit_cast(bf16x8_t, pp[n][ks][i]), acc[d], 0, 0, 0);
                     }
                 }
             }
+        if constexpr (EXACT) reads_ahead<NS * 2 * DB * Kind::kC, products(Kind::kP, Kind::kC) / Kind::kC, 2>();
         // Values that are no finite numbers were left out of the products (0 * infinity would reach the rows that do not see them): they are added as they
         // are to the rows that do.
         if constexpr (!Kind::kScaled) {
@@ -597,24 +691,31 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     if (tid < L::kBufs) s_bad[tid] = 0;
     if (from < to) fetch(from);
     __syncthreads();
-    if constexpr (L::kBufs == 2) {
-        if (from < to) put(from, 0);
-        for (int t = from; t < to; ++t) {
-            const int buf = (t - from) & 1;
-            __syncthreads();
-            advance(t * L::kParts16);
-            if (t + 1 < to) fetch(t + 1);
-            if (t * TT < most) step(t, buf);
-            if (t + 1 < to) put(t + 1, buf ^ 1);
-        }
-    } else {
-        for (int t = from; t < to; ++t) {
-            put(t, 0);
-            __syncthreads();
-            advance(t * L::kParts16);
-            if (t + 1 < to) fetch(t + 1);
-            if (t * TT < most) step(t, 0);
-            __syncthreads();
+    {
+        auto step = [&](int t, int buf) {
+            scores(t, buf);
+            soften(t, buf);
+            product(t, buf);
+        };
+        if constexpr (L::kBufs == 2) {
+            if (from < to) put(from, 0);
+            for (int t = from; t < to; ++t) {
+                const int buf = (t - from) & 1;
+                __syncthreads();
+                advance(t * L::kParts16);
+                fetch(t + 1);
+                if (t * TT < most) step(t, buf);
+                put(t + 1, buf ^ 1);
+            }
+        } else {
+            for (int t = from; t < to; ++t) {
+                put(t, 0);
+                __syncthreads();
+                advance(t * L::kParts16);
+                fetch(t + 1);
+                if (t * TT < most) step(t, 0);
+                __syncthreads();
+            }
         }
     }
     l = xor_add<32>(l);
@@ -647,7 +748,7 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     }
     if (row >= rows) return;
     if (line.parts > 1) {
-        const int64_t slot = (int64_t)work * L::kRows + wr * kCol + c;
+        const int64_t slot = ((int64_t)item * a.pool.n_kv + kv) * L::kRows + wr * kCol + c;
         if (h == 0) *reinterpret_cast<float2 *>(a.stats + slot * 2) = make_float2(m, l);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -674,25 +775,44 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
         }
 }
 
-// Joins the blocks that were cut.  Workgroups stand for the line's parts, of which the first of a block does the work (x), cut by y; a thread stands for four
-// dimensions of a row.
+// Joins the blocks that were cut.  Workgroups stand for blocks of rows (x), cut by y; a thread stands for four dimensions of a row.
 template <typename Row, int kRows, int kTile>
 __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, kv = blockIdx.z;
     Line<kRows, kTile> line(a, lane);
-    const int work = blockIdx.x;
-    if (work >= min((int64_t)line.items * a.pool.n_kv, (int64_t)a.most)) return;
-    const int kv = work / line.items;
-    line.find(a, work % line.items, lane);
-    if (line.part != 0 || line.parts == 1) return;
+    // the x-th of those that are cut: the first part of each block is its place in the line
+    int n = 0;
+    {
+        int at = blockIdx.x;
+        for (int base = 0; base < a.n_seq; base += 64) {
+            const bool few = a.n_seq <= 64, in = base + lane < a.n_seq;
+            Sequence s = few ? line.own : sequence(a, min(base + lane, a.n_seq - 1));
+            const int parts = s.parts(kTile, line.per), blocks = in || few ? s.blocks(a.group, kRows) : 0;
+            const int cut = parts > 1 ? blocks : 0, cut_end = upto(cut, lane), cuts_all = __builtin_amdgcn_readlane(cut_end, 63);
+            const int end = upto(blocks * parts, lane);
+            if (at < cuts_all) {
+                const int l = min((int)__popcll(__ballot(cut_end <= at)), 63);
+                n += __builtin_amdgcn_readlane(end - blocks * parts, l) + (at - __builtin_amdgcn_readlane(cut_end - cut, l)) * __builtin_amdgcn_readlane(parts, l);
+                at = -1;
+                break;
+            }
+            at -= cuts_all;
+            n += __builtin_amdgcn_readlane(end, 63);
+        }
+        if (at >= 0 || n >= line.items) return;
+    }
+    line.find(a, n, lane);
     const int row0 = line.block * kRows, count = min(line.seq.fresh * a.group - row0, kRows), quads = a.D / 4;
     for (int i = blockIdx.y * 256 + threadIdx.x; i < count * quads; i += gridDim.y * 256) {
         const int r = i / quads, q = i - r * quads;
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p = 0; p < line.parts && work + p < a.slots; ++p) {
-            const int64_t slot = (int64_t)(work + p) * kRows + r;
+#pragma unroll 4
+        for (int p = 0; p < line.parts; ++p) {
+            const int64_t place = (int64_t)(n + p) * a.pool.n_kv + kv;
+            if (place >= a.most) break;
+            const int64_t slot = place * kRows + r;
             const float2 ml = *reinterpret_cast<const float2 *>(a.stats + slot * 2);
             const float4 v = *reinterpret_cast<const float4 *>(a.part + slot * a.D + q * 4);
             const float next = fmaxf(m, ml.x), use = next == -INFINITY ? 0.0f : next;
@@ -726,7 +846,8 @@ template <typename Kind, int DP, bool EXACT, int WR, int WK>
 int launch_rows(ChunkArgs a, hipStream_t s)
 {
     typedef Layout<Kind, DP, WR, WK> L;
-    const int64_t blocks = most_blocks(a, L::kRows);
+    // of a cache head at most: for a call whose starts go back, what is beyond is left out
+    const int64_t heads = a.pool.n_kv, blocks = most_blocks(a, L::kRows);
     int64_t grid = blocks;
     const bool cut = blocks < cuts(L::kRows) && a.max_len > kLeast * L::TT;
     if (cut) {
@@ -738,19 +859,19 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     chunk_attend<Kind, DP, EXACT, WR, WK><<<dim3((unsigned)grid), dim3(L::kThreads), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (!cut) return HALO_OK;
-    chunk_join<typename Kind::Row, L::kRows, L::TT><<<dim3(a.slots, (L::kRows * (a.D / 4) + 1023) / 1024), dim3(256), 0, s>>>(a);
+    chunk_join<typename Kind::Row, L::kRows, L::TT><<<dim3((unsigned)(blocks / heads), (L::kRows * (a.D / 4) + 511) / 512, (unsigned)heads), dim3(256), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 
 template <typename Kind, int DP, bool EXACT>
 int launch_chunk(const ChunkArgs &a, hipStream_t s)
 {
-#ifndef WIDE
-#define WIDE 8
-#endif
-    constexpr int kWide = DP * Kind::kC > 128 ? 4 : WIDE;
+    constexpr int kWide = DP * Kind::kC > 128 ? 4 : 8;
     constexpr int kNarrow = DP * Kind::kC > 512 ? 1 : DP * Kind::kC > 256 ? 2 : 4;      // waves of the same rows that LDS has room for
     if ((int64_t)a.N * a.group <= (int64_t)kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 1, kNarrow>(a, s);
+    if constexpr (kWide == 8) {
+        if ((int64_t)a.N * a.group <= (int64_t)4 * kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 4, 2>(a, s);
+    }
     return launch_rows<Kind, DP, EXACT, kWide, 1>(a, s);
 }
 
