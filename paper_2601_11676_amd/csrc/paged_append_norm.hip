@@ -85,6 +85,24 @@ __device__ __forceinline__ double over_row(double v, int lanes)
     for (int d = 1; d < lanes; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
+// 1 / sqrt(v) and 1 / v of a positive number: the hardware's estimates and two steps of Newton's method each, within a few units of 2^-53.  (sqrt and division by the compiler are some 50
+// instructions each, and a lane has 16 elements.)
+__device__ __forceinline__ float root_inverse(float v) { return 1.0f / sqrtf(v); }
+__device__ __forceinline__ double root_inverse(double v)
+{
+    double r = __builtin_amdgcn_rsq(v);
+    if (!(v > 1e-300 && v < 1e300)) return 1.0 / sqrt(v);            // 0, the ends of the numbers, NaN
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = r + r * 0.5 * __builtin_fma(-v * r, r, 1.0);
+    return r;
+}
+__device__ __forceinline__ double inverse(double v)
+{
+    double r = __builtin_amdgcn_rcp(v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(r, __builtin_fma(-v, r, 1.0), r);
+    return r;
+}
 // Largest magnitude, by its bits: infinity and NaN are above every number.
 __device__ __forceinline__ double top_of_row(double v, int lanes)
 {
@@ -114,7 +132,7 @@ struct HeadRow {
         C sum = (C)0;
 #pragma unroll
         for (int i = 0; i < E; ++i) sum += x[i] * x[i] + y[i] * y[i];
-        const C by = (C)1 / sqrt(over_row(sum, a.lanes) / (C)a.D + (C)a.eps);
+        const C by = root_inverse(over_row(sum, a.lanes) * ((C)1 / (C)a.D) + (C)a.eps);
         C u[E], v[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) u[i] = v[i] = (C)1;
@@ -164,11 +182,12 @@ struct HeadRow {
         }
         top = top_of_row(top, lanes);
         const bool number = top < (double)INFINITY;
-        const double step = top / 127.0, by = top > 0.0 && number ? 127.0 / top : 0.0;
+        // rows whose largest is below the normal floats (their scale has hardly a bit) by a quotient
+        const double by = !(top > 0.0 && number) ? 0.0 : top > 0x1p-140 ? 127.0 * inverse(top) : 127.0 / top;
         auto code = [&](double z) {
             const double w = z * by;
             double c = rint(w);
-            if (fabs(w - c) > 0.5 - 1e-6) c = rint(z / step);
+            if (fabs(w - c) > 0.5 - 1e-6) c = rint(z / (top / 127.0));
             return (uint32_t)(uint8_t)(int8_t)(int)(number ? c : 0.0);
         };
         auto put = [&](const C (&z)[E], int e) {
@@ -185,7 +204,7 @@ struct HeadRow {
         put(x, e0);
         put(y, e1);
         if (!first) return;
-        float s = number ? (float)step : NAN;
+        float s = number ? (float)(top / 127.0) : NAN;
         if (number && 127.0f * s == INFINITY) s = __uint_as_float(__float_as_uint(s) - 1);      // or the largest float would read back as infinity
         *scale = s;
     }
@@ -227,34 +246,37 @@ __global__ __launch_bounds__(kThreads) void append_norm_kernel(NormAppendArgs a)
         }
         return;
     }
-    auto compute = [&](auto &r) {
+    const int64_t cell = paged_row(a.pool, page, head, pos);
+    auto compute = [&](auto &r, const T *w) {        // of a query or a key
         r.zero();
         if (in) r.load(source, e0, e1);
-        if (a.norm) {
-            auto normed = r;
-            normed.norm(a, static_cast<const T *>(query ? a.w_q : a.w_k), e0, e1, in && !value);
-            if (!value) r = normed;
-        }
-        if (a.rope && !value && in) r.turn(a, pos, e0, e1, faced);
+        if (a.norm) r.norm(a, w, e0, e1, in);
+        if (a.rope && in) r.turn(a, pos, e0, e1, faced);
     };
-    const int64_t cell = paged_row(a.pool, page, head, pos);
-    if constexpr (Q8) {
-        HeadRow<T, double> r;
-        compute(r);
-        if (query && in) {
-            store_piece<PASS>(q_out + e0, r.x);
-            store_piece<PASS>(q_out + e1, r.y);
-        }
-        r.store_codes(static_cast<int8_t *>(value ? a.v_pages : a.k_pages) + cell * a.D, (value ? a.v_scales : a.k_scales) + cell, a.lanes, e0, e1,
-                      in && !query, in && !query && place == 0);
-    } else {
+    // all lanes of a row take the same way
+    if (query || !Q8) {
         HeadRow<T, float> r;
-        compute(r);
+        if (value) {
+            r.zero();
+            if (in) r.load(source, e0, e1);
+        } else {
+            compute(r, static_cast<const T *>(query ? a.w_q : a.w_k));
+        }
         T *to = query ? q_out : static_cast<T *>(value ? a.v_pages : a.k_pages) + cell * a.D;
         if (in) {
             store_piece<PASS>(to + e0, r.x);
             store_piece<PASS>(to + e1, r.y);
         }
+    } else {
+        HeadRow<T, double> r;
+        if (value) {
+            r.zero();
+            if (in) r.load(source, e0, e1);
+        } else {
+            compute(r, static_cast<const T *>(a.w_k));
+        }
+        r.store_codes(static_cast<int8_t *>(value ? a.v_pages : a.k_pages) + cell * a.D, (value ? a.v_scales : a.k_scales) + cell, a.lanes, e0, e1, in,
+                      in && place == 0);
     }
 }
 

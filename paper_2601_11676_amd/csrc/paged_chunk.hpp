@@ -35,7 +35,7 @@ constexpr int kCol = 32;                             // columns of the matrix in
 constexpr int kLeast = 2;                            // tiles of a part at least
 constexpr int kDies = 8;
 // Parts that few blocks of so many rows are cut into, about: what is resident at once.
-constexpr int cuts(int rows) { return rows >= 256 ? 256 : 512; }
+constexpr int cuts(int rows) { return rows > kCol ? 256 : 512; }
 constexpr int kPartRows = 2 * 256 * 8 * kCol;        // rows of partial results: a part for each cut and one more for each block, fewer than cuts
 static_assert(2 * cuts(kCol) * kCol <= kPartRows, "of narrow blocks too");
 
@@ -172,20 +172,15 @@ __device__ __forceinline__ void query_parts(const float *p, u32x4 (&out)[3])
     parts_of<3>(x, out);
 }
 
-// Wave-wide scans: a lane stands for a sequence.
-__device__ __forceinline__ int upto(int v, int lane)
+// The sum of the lanes up to each one.
+__device__ __forceinline__ int upto(int v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
-__device__ __forceinline__ int64_t over_lanes(int64_t v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor((long long)v, d);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within 16 lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31: the rows before
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
     return v;
 }
 __device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -234,20 +229,19 @@ struct Line {
             own.len = __builtin_amdgcn_ds_permute(to, own.len);
         }
         if (a.slots > 0) {
-            int64_t all = 0;
-            if (few) {
-                all = (int64_t)own.blocks(a.group, kRows) * own.tiles(kTile);
-            } else {
-                for (int i = lane; i < a.n_seq; i += 64) {
-                    const Sequence s = sequence(a, i);
-                    all += (int64_t)s.blocks(a.group, kRows) * s.tiles(kTile);
-                }
+            // tiles of all blocks, and blocks: a part is that share of them that leaves about as many parts as are resident at once (each block's last is half of one)
+            float tiles = 0.0f, blocks = 0.0f;
+            for (int i = lane; i < a.n_seq; i += 64) {
+                const Sequence s = few ? own : sequence(a, i);
+                blocks += (float)s.blocks(a.group, kRows);
+                tiles += (float)s.blocks(a.group, kRows) * (float)s.tiles(kTile);
             }
-            all = over_lanes(all) * a.pool.n_kv;
-            per = same((int)max((all + cuts(kRows) - 1) / cuts(kRows), (int64_t)kLeast));
+            tiles = wave_sum(tiles) * a.pool.n_kv;
+            blocks = wave_sum(blocks) * a.pool.n_kv;
+            per = same(max((int)fminf(tiles / fmaxf(cuts(kRows) - 0.5f * blocks, 0.25f * cuts(kRows)), 1e9f) + 1, kLeast));
         }
         if (few) {
-            end = upto(own.blocks(a.group, kRows) * own.parts(kTile, per), lane);
+            end = upto(own.blocks(a.group, kRows) * own.parts(kTile, per));
             items = __builtin_amdgcn_readlane(end, 63);
         } else {
             for (int base = 0; base < a.n_seq; base += 64) {
@@ -256,7 +250,7 @@ struct Line {
                     const Sequence s = sequence(a, base + lane);
                     mine = s.blocks(a.group, kRows) * s.parts(kTile, per);
                 }
-                items = min(items + __builtin_amdgcn_readlane(upto(mine, lane), 63), a.most);
+                items = min(items + __builtin_amdgcn_readlane(upto(mine), 63), a.most);
             }
         }
         items = min(items, a.most);
@@ -281,7 +275,7 @@ struct Line {
             int mine = 0;
             const Sequence s = sequence(a, min(base + lane, a.n_seq - 1));
             if (base + lane < a.n_seq) mine = s.blocks(a.group, kRows) * s.parts(kTile, per);
-            const int last = upto(mine, lane), all = __builtin_amdgcn_readlane(last, 63);
+            const int last = upto(mine), all = __builtin_amdgcn_readlane(last, 63);
             if (n >= all && base + 64 < a.n_seq) {
                 n -= all;
                 continue;
@@ -789,8 +783,8 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
             const bool few = a.n_seq <= 64, in = base + lane < a.n_seq;
             Sequence s = few ? line.own : sequence(a, min(base + lane, a.n_seq - 1));
             const int parts = s.parts(kTile, line.per), blocks = in || few ? s.blocks(a.group, kRows) : 0;
-            const int cut = parts > 1 ? blocks : 0, cut_end = upto(cut, lane), cuts_all = __builtin_amdgcn_readlane(cut_end, 63);
-            const int end = upto(blocks * parts, lane);
+            const int cut = parts > 1 ? blocks : 0, cut_end = upto(cut), cuts_all = __builtin_amdgcn_readlane(cut_end, 63);
+            const int end = upto(blocks * parts);
             if (at < cuts_all) {
                 const int l = min((int)__popcll(__ballot(cut_end <= at)), 63);
                 n += __builtin_amdgcn_readlane(end - blocks * parts, l) + (at - __builtin_amdgcn_readlane(cut_end - cut, l)) * __builtin_amdgcn_readlane(parts, l);
