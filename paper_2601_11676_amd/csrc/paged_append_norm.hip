@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.hpp"
 #include "paged_index.hpp"
@@ -32,7 +33,7 @@ struct NormAppendArgs {
     int64_t q_stride, k_stride, v_stride;
     PagePool pool;
     int n_heads, D, max_pages, n_seq, max_pos, rotary, pairs, norm;
-    int lanes;                                       // of a row
+    int lanes, lanes_log;                            // of a row, a power of two
     float eps;
     int first;                                       // token of the launch's first workgroup
 };
@@ -103,13 +104,28 @@ __device__ __forceinline__ double inverse(double v)
     for (int i = 0; i < 2; ++i) r = __builtin_fma(r, __builtin_fma(-v, r, 1.0), r);
     return r;
 }
-// Largest magnitude, by its bits: infinity and NaN are above every number.
+__device__ __forceinline__ float top_of_row(float v, int lanes)
+{
+    auto as_f = [](int i) { return __builtin_bit_cast(float, i); };
+    auto other = [&](float f, auto ctrl) { return as_f(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, f), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    if (lanes > 1) v = fmaxf(v, other(v, std::integral_constant<int, 0xB1>{}));          // lane ^ 1, 2 (quad permutations), 4 (half a row's mirror, quads reversed), 8
+    if (lanes > 2) v = fmaxf(v, other(v, std::integral_constant<int, 0x4E>{}));
+    if (lanes > 4) v = fmaxf(v, other(other(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{}));
+    if (lanes > 8) v = fmaxf(v, other(v, std::integral_constant<int, 0x128>{}));
+    if (lanes > 16) v = fmaxf(v, __shfl_xor(v, 16));
+    return v;
+}
 __device__ __forceinline__ double top_of_row(double v, int lanes)
 {
-    unsigned long long u = __double_as_longlong(fabs(v));
-    for (int d = 1; d < lanes; d <<= 1) u = max(u, (unsigned long long)__shfl_xor((long long)u, d));
-    return __longlong_as_double(u);
+    for (int d = 1; d < lanes; d <<= 1) v = fmax(v, __shfl_xor(v, d));
+    return v;
 }
+__device__ __forceinline__ float nearest(float v) { return rintf(v); }
+__device__ __forceinline__ double nearest(double v) { return rint(v); }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ float size(float v) { return fabsf(v); }
+__device__ __forceinline__ double size(double v) { return fabs(v); }
 
 // A head's row in registers: pieces at elements e0 and e1 of lane `place`, normed and turned.
 template <typename T, typename C>
@@ -171,40 +187,56 @@ struct HeadRow {
             }
         }
     }
-    // as codes: what an exact quotient gives, also where the product with 127 / max falls next to the border of two
+    // As codes.  A product with 127 / max says which, unless it lies so near the border of two that its error decides: within 2e-5 in float (two roundings of a number
+    // up to 127, 127 * 2^-23) and 1e-6 in double.  A lane that has one of those takes exact quotients.
     __device__ __forceinline__ void store_codes(int8_t *row, float *scale, int lanes, int e0, int e1, bool in, bool first) const
     {
-        double top = 0.0;
+        C top = (C)0, odd = (C)0;                    // 0 times an infinity or NaN is NaN
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const unsigned long long u = __double_as_longlong(fabs((double)x[i])), v = __double_as_longlong(fabs((double)y[i]));
-            top = __longlong_as_double(max((unsigned long long)__double_as_longlong(top), max(u, v)));
+            top = larger(top, larger(size(x[i]), size(y[i])));
+            odd += x[i] * (C)0 + y[i] * (C)0;
         }
-        top = top_of_row(top, lanes);
-        const bool number = top < (double)INFINITY;
-        // rows whose largest is below the normal floats (their scale has hardly a bit) by a quotient
-        const double by = !(top > 0.0 && number) ? 0.0 : top > 0x1p-140 ? 127.0 * inverse(top) : 127.0 / top;
-        auto code = [&](double z) {
-            const double w = z * by;
-            double c = rint(w);
-            if (fabs(w - c) > 0.5 - 1e-6) c = rint(z / (top / 127.0));
-            return (uint32_t)(uint8_t)(int8_t)(int)(number ? c : 0.0);
-        };
-        auto put = [&](const C (&z)[E], int e) {
-            uint32_t w[E / 4];
+        top = top_of_row(odd == (C)0 ? top : (C)INFINITY, lanes);
+        const bool number = top < (C)INFINITY, few = !(top >= (C)0x1p-100);      // few: a product could overflow
+        const double step = (double)top * (1.0 / 127.0);
+        const C by = few || !number ? (C)0 : (C)(127.0 * inverse((double)top)), border = sizeof(C) == 4 ? (C)(0.5 - 2e-5) : (C)(0.5 - 1e-6);
+        C far = (C)0;
+        uint32_t w[2][E / 4];
+        auto put = [&](const C (&z)[E], uint32_t (&words)[E / 4]) {
 #pragma unroll
-            for (int i = 0; i < E / 4; ++i)
-                w[i] = code(z[4 * i]) | code(z[4 * i + 1]) << 8 | code(z[4 * i + 2]) << 16 | code(z[4 * i + 3]) << 24;
-            if (!in) return;
-            if constexpr (E == 8)
-                *reinterpret_cast<uint2 *>(row + e) = make_uint2(w[0], w[1]);
-            else
-                *reinterpret_cast<uint32_t *>(row + e) = w[0];
+            for (int i = 0; i < E; ++i) {
+                const C v = z[i] * by, c = nearest(v);
+                far = larger(far, size(v - c));
+                const uint32_t code = (uint32_t)(uint8_t)(int)c;
+                words[i / 4] = i % 4 ? words[i / 4] | code << (8 * (i % 4)) : code;
+            }
         };
-        put(x, e0);
-        put(y, e1);
+        put(x, w[0]);
+        put(y, w[1]);
+        if (!number) {
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i) w[0][i] = w[1][i] = 0;
+        } else if ((far > border || few) && top > (C)0) {
+            const double exact = (double)top / 127.0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const uint32_t u = (uint32_t)(uint8_t)(int)rint((double)x[i] / exact), v = (uint32_t)(uint8_t)(int)rint((double)y[i] / exact);
+                w[0][i / 4] = i % 4 ? w[0][i / 4] | u << (8 * (i % 4)) : u;
+                w[1][i / 4] = i % 4 ? w[1][i / 4] | v << (8 * (i % 4)) : v;
+            }
+        }
+        if (in) {
+            if constexpr (E == 8) {
+                *reinterpret_cast<uint2 *>(row + e0) = make_uint2(w[0][0], w[0][1]);
+                *reinterpret_cast<uint2 *>(row + e1) = make_uint2(w[1][0], w[1][1]);
+            } else {
+                *reinterpret_cast<uint32_t *>(row + e0) = w[0][0];
+                *reinterpret_cast<uint32_t *>(row + e1) = w[1][0];
+            }
+        }
         if (!first) return;
-        float s = number ? (float)(top / 127.0) : NAN;
+        float s = number ? (float)step : NAN;
         if (number && 127.0f * s == INFINITY) s = __uint_as_float(__float_as_uint(s) - 1);      // or the largest float would read back as infinity
         *scale = s;
     }
@@ -214,8 +246,8 @@ template <typename T, bool Q8, bool PASS>
 __global__ __launch_bounds__(kThreads) void append_norm_kernel(NormAppendArgs a)
 {
     constexpr int E = kElems<T>;
-    const int token = a.first + blockIdx.x, places = a.D / (2 * E), at_once = kThreads / a.lanes;
-    const int place = threadIdx.x % a.lanes, row = threadIdx.x / a.lanes + blockIdx.y * at_once;
+    const int token = a.first + blockIdx.x, places = a.D / (2 * E);
+    const int place = threadIdx.x & (a.lanes - 1), row = (threadIdx.x >> a.lanes_log) + blockIdx.y * (kThreads >> a.lanes_log);
     const int k_from = a.q ? a.n_heads : 0, v_from = k_from + a.pool.n_kv, rows = v_from + a.pool.n_kv;
     const bool in = row < rows && place < places;    // the others stay for the exchanges
 
@@ -268,15 +300,18 @@ __global__ __launch_bounds__(kThreads) void append_norm_kernel(NormAppendArgs a)
             store_piece<PASS>(to + e1, r.y);
         }
     } else {
-        HeadRow<T, double> r;
-        if (value) {
+        int8_t *to = static_cast<int8_t *>(value ? a.v_pages : a.k_pages) + cell * a.D;
+        float *scale = (value ? a.v_scales : a.k_scales) + cell;
+        if (value || (!a.norm && !a.rope)) {         // rows as they came, exact as floats
+            HeadRow<T, float> r;
             r.zero();
             if (in) r.load(source, e0, e1);
+            r.store_codes(to, scale, a.lanes, e0, e1, in, in && place == 0);
         } else {
+            HeadRow<T, double> r;
             compute(r, static_cast<const T *>(a.w_k));
+            r.store_codes(to, scale, a.lanes, e0, e1, in, in && place == 0);
         }
-        r.store_codes(static_cast<int8_t *>(value ? a.v_pages : a.k_pages) + cell * a.D, (value ? a.v_scales : a.k_scales) + cell, a.lanes, e0, e1, in,
-                      in && place == 0);
     }
 }
 
@@ -355,7 +390,7 @@ int append(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_st
     a.rotary = rope ? rotary_dim : 0;
     a.pairs = rope_pairs != 0;
     a.lanes = 1;
-    while (a.lanes * 32 < s.head_dim * size) a.lanes *= 2;
+    while (a.lanes * 32 < s.head_dim * size) a.lanes *= 2, ++a.lanes_log;
     const int at_once = kThreads / a.lanes, rows = (q ? s.n_heads : 0) + 2 * s.n_kv_heads;
     // stores with the non-temporal hint where they fill whole 64-byte parts of lines and are many, as in paged_append.hip
     const int faced = rope && !rope_pairs ? rotary_dim : 0;

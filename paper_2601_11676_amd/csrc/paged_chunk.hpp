@@ -309,9 +309,9 @@ template <typename Kind, int DP, int WR, int WK>
 struct Layout {
     typedef typename Kind::Cell Cell;
     static constexpr int kRows = WR * kCol, kWaves = WR * WK, kThreads = kWaves * 64;
-    static constexpr int TT = WK > 1 ? WK * 32 : DP * Kind::kC > 256 ? 32 : 64, kSub = TT / 32 / WK;
+    static constexpr int TT = WK > 1 ? WK * 32 : DP * Kind::kC > 128 ? 32 : 64, kSub = TT / 32 / WK;
     static constexpr int kPlane = TT * DP * 2, kTileBytes = 2 * Kind::kC * kPlane, kJoin = (WK - 1) * kRows * (DP + 2) * 4;
-    static constexpr int kBufs = kTileBytes <= 65536 ? 2 : 1, kRowsBytes = kTileBytes / 2;
+    static constexpr int kBufs = kTileBytes <= 65536 && WK < 4 ? 2 : 1, kRowsBytes = kTileBytes / 2;
     static constexpr int kLds = kBufs * kTileBytes > kJoin ? kBufs * kTileBytes : kJoin;
     // loads of a wave, 1 KiB each: of kRowsEach rows, which lie in one part of 16 tokens
     static constexpr int kRowBytes = DP * (int)sizeof(Cell), kRowLanes = kRowBytes / 16, kRowsEach = 64 / kRowLanes, kLoads = TT / kRowsEach;
@@ -860,11 +860,14 @@ int launch_rows(ChunkArgs a, hipStream_t s)
 template <typename Kind, int DP, bool EXACT>
 int launch_chunk(const ChunkArgs &a, hipStream_t s)
 {
-    constexpr int kWide = DP * Kind::kC > 128 ? 4 : 8;
-    constexpr int kNarrow = DP * Kind::kC > 512 ? 1 : DP * Kind::kC > 256 ? 2 : 4;      // waves of the same rows that LDS has room for
-    if ((int64_t)a.N * a.group <= (int64_t)kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 1, kNarrow>(a, s);
+    // waves of a wide block: of eight a SIMD has two, 256 registers each, which long rows and rows of three parts pass
+    constexpr int kWide = DP * (Kind::kC > Kind::kQ ? Kind::kC : Kind::kQ) > 128 ? 4 : 8;
+    const int64_t rows = (int64_t)a.N * a.group;     // against those of all sequences in even blocks
+    if constexpr (DP <= 128 && DP * Kind::kC <= 256) {       // four waves that share rows: LDS and registers for 128 tokens
+        if (rows <= (int64_t)kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 1, 4>(a, s);
+    }
     if constexpr (kWide == 8) {
-        if ((int64_t)a.N * a.group <= (int64_t)4 * kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 4, 2>(a, s);
+        if (rows <= (int64_t)4 * kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 4, 2>(a, s);
     }
     return launch_rows<Kind, DP, EXACT, kWide, 1>(a, s);
 }
