@@ -19,13 +19,15 @@ namespace {
 inline size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kMostSeqs = 4096, kMostTokens = 1 << 21;
 
-// What cut blocks leave.
+// What cut blocks leave, and with a mask the rows that survive.
 struct ChunkWorkspace {
-    size_t part = 0, bytes = 0;
-    ChunkWorkspace(const halo_paged_shape &s)
+    size_t part = 0, kept = 0, n_kept = 0, bytes = 0;
+    ChunkWorkspace(const halo_paged_shape &s, int N, int n_seq)
     {
         part = align256((size_t)kPartRows * 2 * sizeof(float));
-        bytes = part + align256((size_t)kPartRows * s.head_dim * sizeof(float));
+        kept = part + align256((size_t)kPartRows * s.head_dim * sizeof(float));
+        n_kept = kept + align256((size_t)N * s.n_heads * sizeof(int32_t));
+        bytes = n_kept + align256((size_t)n_seq * s.n_kv_heads * sizeof(int32_t));
     }
 };
 
@@ -44,7 +46,7 @@ int chunk(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_str
     if (q_stride < (int64_t)s.n_heads * s.head_dim || q_stride * size % 16 || odd(q, 16) || odd(k, 16) || odd(v, 16) || odd(out, 16) ||
         odd(workspace, 16) || odd(k_scale, 4) || odd(v_scale, 4) || odd(starts, 4) || odd(table, 4) || odd(lens, 4))
         return HALO_ERR_ARG;
-    const ChunkWorkspace ws(s);
+    const ChunkWorkspace ws(s, N, n_seq);
     if (!workspace || ws_bytes < ws.bytes) return HALO_ERR_WORKSPACE;
 
     ChunkArgs a{};
@@ -52,6 +54,8 @@ int chunk(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_str
     a.starts = starts; a.table = table; a.lens = lens; a.mask = mask; a.out = out;
     a.stats = static_cast<float *>(workspace);
     a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + ws.part);
+    a.kept = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + ws.kept);
+    a.n_kept = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + ws.n_kept);
     a.q_stride = q_stride;
     a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
     a.N = N; a.n_seq = n_seq; a.n_heads = s.n_heads; a.group = s.n_heads / s.n_kv_heads; a.D = s.head_dim;
@@ -69,7 +73,7 @@ extern "C" size_t halo_paged_chunk_workspace_bytes(const halo_paged_shape *shape
 {
     using namespace halo;
     if (check_paged_shape(shape) != HALO_OK || N < 0 || N > kMostTokens || n_seq < 0 || n_seq > kMostSeqs) return 0;
-    return ChunkWorkspace(*shape).bytes;
+    return ChunkWorkspace(*shape, N, n_seq).bytes;
 }
 
 extern "C" int halo_paged_chunk_attention(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k_pages,

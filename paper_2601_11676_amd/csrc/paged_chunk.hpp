@@ -9,9 +9,6 @@
 #include "kernels.hpp"
 #include "paged_index.hpp"
 
-#ifndef AHEAD
-#define AHEAD 4
-#endif
 namespace halo {
 
 struct ChunkArgs {
@@ -21,6 +18,7 @@ struct ChunkArgs {
     const uint8_t *mask;
     void *out;
     float *part, *stats;                             // partial results of cut blocks: [slot][rows][D], [slot][rows][max, sum]
+    int32_t *kept, *n_kept;                          // with a mask: rows that survive [cache head][N * group] and how many [cache head][sequence] (chunk_rows)
     int64_t q_stride;
     PagePool pool;
     int N, n_seq, n_heads, group, D, max_pages, max_len;
@@ -296,6 +294,23 @@ __device__ __forceinline__ bool place_of(const ChunkArgs &a, int block, int item
     return item < items && (int64_t)item * a.pool.n_kv + kv < a.most;
 }
 
+// The rows of a sequence and cache head that the mask keeps, in order: the i-th of them, or of more the last.
+struct Survivors {
+    const int32_t *list;
+    int rows, last;                                  // rows, and the last row of the sequence
+    __device__ __forceinline__ Survivors(const ChunkArgs &a, const Sequence &s, int number, int kv) : list(nullptr), rows(s.fresh * a.group), last(rows - 1)
+    {
+        if (!a.kept) return;
+        list = a.kept + ((int64_t)kv * a.N + s.first) * a.group;
+        rows = same(a.n_kept[(int64_t)kv * a.n_seq + number]);
+    }
+    __device__ __forceinline__ int row(int i) const
+    {
+        i = min(i, rows - 1);
+        return list ? min(list[i], last) : i;        // no further than the sequence, were starts to go back and lists to be one another's
+    }
+};
+
 __device__ __forceinline__ void store_four(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void store_four(bf16_t *p, const float (&v)[4])
 {
@@ -331,12 +346,12 @@ template <int DP> __device__ __forceinline__ int value_place(int row, int piece)
 // Products of parts that are taken.
 constexpr int products(int a, int b) { return a * b < 9 ? a * b : 6; }
 
-// The order of a run of matrix instructions and of the loads from LDS of their operands, READS loads an operand: AHEAD operands first, then one for each that is used up
+// The order of a run of matrix instructions and of the loads from LDS of their operands, READS loads an operand: four operands first, then one for each that is used up
 // (left to itself the compiler loads one ahead and waits out the latency at every second instruction).
 template <int OPERANDS, int MFMAS, int READS>
 __device__ __forceinline__ void reads_ahead()
 {
-    constexpr int kAhead = AHEAD < OPERANDS ? AHEAD : OPERANDS;
+    constexpr int kAhead = OPERANDS < 4 ? OPERANDS : 4;
     __builtin_amdgcn_sched_group_barrier(0x100, kAhead * READS, 0);
 #pragma unroll
     for (int i = 0; i < OPERANDS - kAhead; ++i) {
@@ -365,21 +380,21 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     int item, kv;
     if (!place_of(a, blockIdx.x, line.items, item, kv)) return;
     const int sq = line.find(a, item, lane);
-    const int rows = line.seq.fresh * a.group, row0 = line.block * L::kRows, past = line.seq.len - line.seq.fresh;
+    const Survivors survivors(a, line.seq, sq, kv);
+    const int rows = survivors.rows, row0 = line.block * L::kRows, past = line.seq.len - line.seq.fresh;
+    if (row0 >= rows) return;
 
     // the lane's row: a query head of a token, heads first
-    const int row = row0 + wr * kCol + c, there = min(row, rows - 1);
+    const int row = row0 + wr * kCol + c, there = survivors.row(row);
     const int token = there / a.group, head = kv * a.group + (there - token * a.group);
     const int64_t at = line.seq.first + token;
-    const bool kept = !a.mask || a.mask[at * a.n_heads + head] != 0;
-    const int lim = max(past + token + 1, 0);        // positions that it sees
-    const int wave_last = min(row0 + (wr + 1) * kCol, rows) - 1, wave_first = min(row0 + wr * kCol, rows - 1);
-    const int most = row0 + wr * kCol < rows ? same(max(past + wave_last / a.group + 1, 0)) : 0,      // a wave without rows reads nothing
-         least = same(max(past + wave_first / a.group + 1, 0));
-    const int block_most = same(max(past + (min(row0 + L::kRows, rows) - 1) / a.group + 1, 0)), block_least = same(max(past + row0 / a.group + 1, 0));
+    const bool kept = !a.mask || a.kept || a.mask[at * a.n_heads + head] != 0;
+    const int lim = max(past + token + 1, 0);        // positions that it sees; of the wave's rows and of the block's, the most and the least
+    const int most = row0 + wr * kCol < rows ? __builtin_amdgcn_readlane(lim, 31) : 0, least = __builtin_amdgcn_readlane(lim, 0);      // a wave without rows reads nothing
+    const int block_most = same(max(past + survivors.row(row0 + L::kRows - 1) / a.group + 1, 0)), block_least = same(max(past + survivors.row(row0) / a.group + 1, 0));
     int tiles = (block_most + TT - 1) / TT;
     // a block without a row that counts reads nothing
-    if (a.mask && !__syncthreads_or(kept && row < rows)) tiles = 0;
+    if (a.mask && !a.kept && !__syncthreads_or(kept && row < rows)) tiles = 0;
     const int from = same((int)((int64_t)tiles * line.part / line.parts)), to = same((int)((int64_t)tiles * (line.part + 1) / line.parts));
 
     // page numbers of the parts of 16 tokens, 64 parts at a time, a lane each (-1: no page), and which are pages
@@ -796,8 +811,9 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
         }
         if (at >= 0 || n >= line.items) return;
     }
-    line.find(a, n, lane);
-    const int row0 = line.block * kRows, count = min(line.seq.fresh * a.group - row0, kRows), quads = a.D / 4;
+    const int sq = line.find(a, n, lane);
+    const Survivors survivors(a, line.seq, sq, kv);
+    const int row0 = line.block * kRows, count = min(survivors.rows - row0, kRows), quads = a.D / 4;
     for (int i = blockIdx.y * 256 + threadIdx.x; i < count * quads; i += gridDim.y * 256) {
         const int r = i / quads, q = i - r * quads;
         float m = -INFINITY, l = 0.0f;
@@ -818,12 +834,64 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
             o.w = o.w * keep + v.w * by;
             m = next;
         }
-        const int row = row0 + r, token = row / a.group, head = kv * a.group + (row - token * a.group);
+        const int row = survivors.row(row0 + r), token = row / a.group, head = kv * a.group + (row - token * a.group);
         const int64_t at = line.seq.first + token;
         const bool none = m == -INFINITY || (a.mask && !a.mask[at * a.n_heads + head]);
         const float by = 1.0f / l;
         const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
         store_four(static_cast<Row *>(a.out) + (at * a.n_heads + head) * a.D + q * 4, v);
+    }
+}
+
+// With a mask, before the others: lists the rows that survive, so that blocks are of those alone, and gives 0 to the rest.  Workgroups stand for a sequence, a cache head
+// and kScan of its rows; each counts the survivors before its own.
+constexpr int kScan = 512;
+template <typename Row>
+__global__ __launch_bounds__(256) void chunk_rows(ChunkArgs a)
+{
+    constexpr int kEach = kScan / 256;
+    __shared__ int s_count[4 * kEach];
+    __shared__ uint64_t s_bits[4 * kEach];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kv = blockIdx.y;
+    const Sequence s = sequence(a, blockIdx.x);
+    const int rows = s.fresh * a.group, row0 = blockIdx.z * kScan;
+    if (row0 >= rows && row0 > 0) return;
+    const uint8_t *mask = a.mask + (int64_t)s.first * a.n_heads + kv * a.group;
+    auto kept = [&](int r) {
+        if (r >= rows) return false;
+        const int token = r / a.group;
+        return mask[(int64_t)token * a.n_heads + (r - token * a.group)] != 0;
+    };
+    int before = 0;
+#pragma unroll 8
+    for (int r = tid; r < row0; r += 256) before += kept(r);
+    before = (int)wave_sum((float)before);           // at most 2^24 / 4 rows a wave
+    if (lane == 0) s_count[wave] = before;
+    __syncthreads();
+    before = s_count[0] + s_count[1] + s_count[2] + s_count[3];
+    __syncthreads();
+    bool mine[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        mine[i] = kept(row0 + i * 256 + tid);
+        const uint64_t bits = __ballot(mine[i]);
+        if (lane == 0) s_count[i * 4 + wave] = __popcll(bits), s_bits[i * 4 + wave] = bits;
+    }
+    __syncthreads();
+    int32_t *list = a.kept + ((int64_t)kv * a.N + s.first) * a.group;
+    int place = before;
+#pragma unroll
+    for (int i = 0; i < 4 * kEach; ++i) {
+        if (i % 4 == wave && mine[i / 4]) list[place + __popcll(s_bits[i] & ((1ull << lane) - 1))] = row0 + i / 4 * 256 + tid;
+        place += s_count[i];
+    }
+    if (tid == 0 && row0 + kScan >= rows) a.n_kept[(int64_t)kv * a.n_seq + blockIdx.x] = place;
+    const int pieces = a.D * (int)sizeof(Row) / 16, count = min(rows - row0, kScan);
+    for (int r = tid >> 4; r < count; r += 16) {     // 16 lanes a row
+        if ((s_bits[r / 64] >> (r & 63)) & 1) continue;
+        const int token = (row0 + r) / a.group;
+        Row *out = static_cast<Row *>(a.out) + ((int64_t)(s.first + token) * a.n_heads + kv * a.group + (row0 + r - token * a.group)) * a.D;
+        for (int piece = tid & 15; piece < pieces; piece += 16) reinterpret_cast<u32x4 *>(out)[piece] = u32x4{0u, 0u, 0u, 0u};
     }
 }
 
@@ -850,6 +918,16 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     }
     a.most = (int)grid;
     grid = (grid + kDies - 1) / kDies * kDies;
+    // Blocks of the surviving rows alone save their share of the products, and cost a launch and blocks that end where their sequence does more often.  us, without / with the list:
+    // 7 sequences of 4099 in all, 40 heads, three quarters of them kept (1.5e8 scores of the longest sequence) 77 / 85; 4 of 4000, 32 heads, half (2e8) 79 / 72; one of 4096 (5e8)
+    // 172 / 147, of 8192 564 / 353, with three quarters 561 / 482; 2 of 4000 after 2000, 64 heads, 8 cache heads, half 372 / 234.
+    if (!a.mask || (int64_t)a.N * a.n_heads * a.max_len < 200000000) {
+        a.kept = nullptr;
+    } else {
+        const int64_t rows = (int64_t)a.N * a.group;
+        chunk_rows<typename Kind::Row><<<dim3(a.n_seq, a.pool.n_kv, (unsigned)((rows + kScan - 1) / kScan)), dim3(256), 0, s>>>(a);
+        if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
+    }
     chunk_attend<Kind, DP, EXACT, WR, WK><<<dim3((unsigned)grid), dim3(L::kThreads), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (!cut) return HALO_OK;
@@ -867,7 +945,11 @@ int launch_chunk(const ChunkArgs &a, hipStream_t s)
         if (rows <= (int64_t)kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 1, 4>(a, s);
     }
     if constexpr (kWide == 8) {
-        if (rows <= (int64_t)4 * kCol * a.n_seq) return launch_rows<Kind, DP, EXACT, 4, 2>(a, s);
+        // Blocks of 128 rows, two waves for the same, where rows are few, and where wide blocks would be one round of unequal ones.  us, 256 rows / 128: 16 sequences of 40 new
+        // tokens after 3000, 64 heads, 8 cache heads (288 blocks) 101 / 93; one of 2048, 32 heads, half kept (288) 80 / 63; 4 of 4000 in all (620) 79 / 98; 7 of 4099, 40 heads (920)
+        // 77 / 103; cut blocks: 4 of 400 in all after 2000 (132) 51 / 55, one of 1024 after 2000 (160) 76 / 72.
+        const int64_t wide = most_blocks(a, 8 * kCol);
+        if (rows <= (int64_t)4 * kCol * a.n_seq || (wide >= 256 && wide < 512)) return launch_rows<Kind, DP, EXACT, 4, 2>(a, s);
     }
     return launch_rows<Kind, DP, EXACT, kWide, 1>(a, s);
 }

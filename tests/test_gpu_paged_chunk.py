@@ -142,6 +142,8 @@ CHUNKS = [
     (4, 4, 128, 16, [(0, 33), (0, 200), (5, 127)], None), (8, 2, 64, 16, [(0, 64), (63, 65), (64, 64), (1, 129)], 0.5), (16, 1, 96, 16, [(40, 60)], None),
     (40, 2, 128, 16, [(1500, 40), (0, 7)], 0.7), (2, 2, 112, 32, [(0, 300)], None), (3, 3, 256, 64, [(100, 150), (0, 33)], None),
     (6, 2, 144, 16, [(9, 90)], 0.4), (5, 1, 208, 16, [(0, 70)], None), (64, 8, 128, 64, [(900, 64)], None), (2, 1, 64, 128, [(0, 1025)], None),
+    # many scores under a mask: the surviving rows are listed first, of blocks whole and cut
+    (64, 64, 16, 16, [(2300, 700), (0, 400)], 0.5), (64, 4, 64, 16, [(2300, 700), (5, 0), (0, 410)], 0.3), (256, 2, 16, 16, [(7900, 100)], 0.4),
     # as many blocks as the card has places: nothing is cut
     (64, 64, 64, 16, [(0, 600), (13, 510)], 0.5), (80, 40, 32, 16, [(0, 300), (0, 500), (100, 90)], None), (128, 128, 16, 32, [(3, 20)] * 20, 0.3),
 ]
@@ -192,6 +194,22 @@ def test_masks_that_leave_nothing(kind, past):
     assert torch.all(got[:16] == 0) and torch.all(got[s[1]:s[2]] == 0) and torch.all((got[31] != 0).any(-1))
     m[:] = 0
     assert torch.all(case.run() == 0)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "q8-f32"])
+def test_listed_rows_that_leave_nothing(kind):
+    # the same where survivors are listed: no row of a cache head, of a sequence, of a block; runs of one
+    case = Case(kind, 64, 4, 32, 16, [(2300, 700), (0, 3), (0, 400)], keep=0.4, seed=16, before=1, behind=2)
+    m, s = case.mask, case.starts.tolist()
+    m[:, :16] = 0
+    m[s[0]:s[0] + 600, 16:32] = 0
+    m[s[0] + 10, 20] = 3
+    m[s[1]:s[2]] = 0
+    got = case.run()
+    case.check(got)
+    assert torch.all(got[s[0]:s[-1], :16] == 0) and torch.all((got[s[0] + 10, 20] != 0).any()) and torch.all(got[:1] == 77) and torch.all(got[-2:] == 77)
+    m[:] = 0
+    assert torch.all(case.run()[1:-2] == 0)
 
 
 @pytest.mark.parametrize("kind", KINDS)
