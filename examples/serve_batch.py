@@ -94,8 +94,7 @@ class Server:
             torch.matmul(b["x"], k.Wqkv.t(), out=b["qkv"])
             heads = b["qkv"].view(-1, c.heads + 2 * c.kv_heads, c.head_dim)
             q, kn, vn = heads[:, :c.heads], heads[:, c.heads:c.heads + c.kv_heads], heads[:, c.heads + c.kv_heads:]
-            H.halo_paged_append(self.shape, q, kn, vn, pos, self.table, k.k_pages, k.v_pages, q_out=b["q"], rope=self.rope, seq=seq)
-            H.halo_paged_attention(self.shape, b["q"], k.k_pages, k.v_pages, rows, lens, max_len, b["o"], b["ws"], mask=b["head_mask"][i])
+            self.attend(b, k, (q, kn, vn), pos, seq, rows, lens, max_len, b["head_mask"][i])
             torch.matmul(b["o"].view(-1, c.heads * c.head_dim), k.Wo.t(), out=b["y"])
             H.halo_block_norm(b["h"], b["y"], b["x"], post_norm=True, gate=k.gate, w_pre=k.w_ffn)
             # FFN of the surviving groups
@@ -104,6 +103,12 @@ class Server:
             after = self.blocks[i + 1].w_attn if i + 1 < len(self.blocks) else k.w_next
             H.halo_block_norm(b["h"], b["y"], b["x"], res_scale=0.9, w_pre=after)
         return b["x"]
+
+    def attend(self, b, k, new, pos, seq, rows, lens, max_len: int, mask):
+        """New queries, keys and values: into block k's cache, and b["o"] from all of it that they may see."""
+        q, kn, vn = new
+        H.halo_paged_append(self.shape, q, kn, vn, pos, self.table, k.k_pages, k.v_pages, q_out=b["q"], rope=self.rope, seq=seq)
+        H.halo_paged_attention(self.shape, b["q"], k.k_pages, k.v_pages, rows, lens, max_len, b["o"], b["ws"], mask=mask)
 
     def room(self, counts):
         """Refuses counts[i] new tokens of sequence i where there is no room for them."""
