@@ -512,7 +512,8 @@ struct CoreQ8 {
     typedef int8_t Cell;
     static constexpr bool kScaled = true;
     static constexpr int QT = TILES;
-    static constexpr int kSub = DP > 128 ? 2 : 4, kTile = kSub * 16;
+    // tokens of a step: 32 of rows of 128, over large caches 64 (us, 64 / 32: one sequence of 32771, 8 cache heads, 25.6 / 22.6; 96 of up to 8192 152 / 155)
+    static constexpr int kSub = DP > 128 || (DP > 64 && HINT != kPassBoth) ? 2 : 4, kTile = kSub * 16;
     static constexpr int kItemWaves = DP > 128 ? 4 : 8, kWaves = DP > 128 || (DP > 64 && QT * QP > 1) ? 1 : 2;
     static constexpr int kSteps = DP > 64 ? 8 : 4, kLeast = DP > 128 ? 4 : 2;
     static constexpr int kMostRows = QT * kCols * DP * 4, kStage = kTile * DP > kMostRows ? kTile * DP : kMostRows;

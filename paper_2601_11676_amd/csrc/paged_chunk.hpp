@@ -843,8 +843,8 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
     }
 }
 
-// With a mask, before the others: lists the rows that survive, so that blocks are of those alone, and gives 0 to the rest.  Workgroups stand for a sequence, a cache head
-// and kScan of its rows; each counts the survivors before its own.
+// With a mask, before the others: lists the rows that survive, so that blocks are of those alone, and gives 0 to the rest.  Workgroups stand for a sequence (x) and a cache
+// head (y); those of one pair (z) take kScan of its rows each in turn, and count the survivors before them.
 constexpr int kScan = 512;
 template <typename Row>
 __global__ __launch_bounds__(256) void chunk_rows(ChunkArgs a)
@@ -854,44 +854,48 @@ __global__ __launch_bounds__(256) void chunk_rows(ChunkArgs a)
     __shared__ uint64_t s_bits[4 * kEach];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kv = blockIdx.y;
     const Sequence s = sequence(a, blockIdx.x);
-    const int rows = s.fresh * a.group, row0 = blockIdx.z * kScan;
-    if (row0 >= rows && row0 > 0) return;
+    const int rows = s.fresh * a.group, pieces = a.D * (int)sizeof(Row) / 16;
     const uint8_t *mask = a.mask + (int64_t)s.first * a.n_heads + kv * a.group;
+    int32_t *list = a.kept + ((int64_t)kv * a.N + s.first) * a.group;
     auto kept = [&](int r) {
         if (r >= rows) return false;
         const int token = r / a.group;
         return mask[(int64_t)token * a.n_heads + (r - token * a.group)] != 0;
     };
-    int before = 0;
+    if (rows == 0 && blockIdx.z == 0 && tid == 0) a.n_kept[(int64_t)kv * a.n_seq + blockIdx.x] = 0;
+    int place = 0, counted = 0;                      // survivors before row `counted`
+    for (int row0 = blockIdx.z * kScan; row0 < rows; row0 += gridDim.z * kScan) {
+        int before = 0;
 #pragma unroll 8
-    for (int r = tid; r < row0; r += 256) before += kept(r);
-    before = (int)wave_sum((float)before);           // at most 2^24 / 4 rows a wave
-    if (lane == 0) s_count[wave] = before;
-    __syncthreads();
-    before = s_count[0] + s_count[1] + s_count[2] + s_count[3];
-    __syncthreads();
-    bool mine[kEach];
+        for (int r = counted + tid; r < row0; r += 256) before += kept(r);
+        before = __builtin_amdgcn_readlane(upto(before), 63);
+        if (lane == 0) s_count[wave] = before;
+        __syncthreads();
+        place += s_count[0] + s_count[1] + s_count[2] + s_count[3];
+        __syncthreads();
+        bool mine[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        mine[i] = kept(row0 + i * 256 + tid);
-        const uint64_t bits = __ballot(mine[i]);
-        if (lane == 0) s_count[i * 4 + wave] = __popcll(bits), s_bits[i * 4 + wave] = bits;
-    }
-    __syncthreads();
-    int32_t *list = a.kept + ((int64_t)kv * a.N + s.first) * a.group;
-    int place = before;
+        for (int i = 0; i < kEach; ++i) {
+            mine[i] = kept(row0 + i * 256 + tid);
+            const uint64_t bits = __ballot(mine[i]);
+            if (lane == 0) s_count[i * 4 + wave] = __popcll(bits), s_bits[i * 4 + wave] = bits;
+        }
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4 * kEach; ++i) {
-        if (i % 4 == wave && mine[i / 4]) list[place + __popcll(s_bits[i] & ((1ull << lane) - 1))] = row0 + i / 4 * 256 + tid;
-        place += s_count[i];
-    }
-    if (tid == 0 && row0 + kScan >= rows) a.n_kept[(int64_t)kv * a.n_seq + blockIdx.x] = place;
-    const int pieces = a.D * (int)sizeof(Row) / 16, count = min(rows - row0, kScan);
-    for (int r = tid >> 4; r < count; r += 16) {     // 16 lanes a row
-        if ((s_bits[r / 64] >> (r & 63)) & 1) continue;
-        const int token = (row0 + r) / a.group;
-        Row *out = static_cast<Row *>(a.out) + ((int64_t)(s.first + token) * a.n_heads + kv * a.group + (row0 + r - token * a.group)) * a.D;
-        for (int piece = tid & 15; piece < pieces; piece += 16) reinterpret_cast<u32x4 *>(out)[piece] = u32x4{0u, 0u, 0u, 0u};
+        for (int i = 0; i < 4 * kEach; ++i) {
+            if (i % 4 == wave && mine[i / 4]) list[place + __popcll(s_bits[i] & ((1ull << lane) - 1))] = row0 + i / 4 * 256 + tid;
+            place += s_count[i];
+        }
+        counted = row0 + kScan;
+        if (tid == 0 && counted >= rows) a.n_kept[(int64_t)kv * a.n_seq + blockIdx.x] = place;
+        const int count = min(rows - row0, kScan);
+        for (int r = tid >> 4; r < count; r += 16) { // 16 lanes a row
+            if ((s_bits[r / 64] >> (r & 63)) & 1) continue;
+            const int token = (row0 + r) / a.group;
+            Row *out = static_cast<Row *>(a.out) + ((int64_t)(s.first + token) * a.n_heads + kv * a.group + (row0 + r - token * a.group)) * a.D;
+            for (int piece = tid & 15; piece < pieces; piece += 16) reinterpret_cast<u32x4 *>(out)[piece] = u32x4{0u, 0u, 0u, 0u};
+        }
+        __syncthreads();                             // before the counts are written again
     }
 }
 
@@ -924,8 +928,9 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     if (!a.mask || (int64_t)a.N * a.n_heads * a.max_len < 200000000) {
         a.kept = nullptr;
     } else {
-        const int64_t rows = (int64_t)a.N * a.group;
-        chunk_rows<typename Kind::Row><<<dim3(a.n_seq, a.pool.n_kv, (unsigned)((rows + kScan - 1) / kScan)), dim3(256), 0, s>>>(a);
+        const int64_t scans = ((int64_t)a.N * a.group + kScan - 1) / kScan, pairs = (int64_t)a.n_seq * heads;
+        const int64_t each = pairs < 2048 ? 2048 / pairs : 1;        // eight workgroups a unit
+        chunk_rows<typename Kind::Row><<<dim3(a.n_seq, (unsigned)heads, (unsigned)(each < scans ? each : scans)), dim3(256), 0, s>>>(a);
         if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     }
     chunk_attend<Kind, DP, EXACT, WR, WK><<<dim3((unsigned)grid), dim3(L::kThreads), 0, s>>>(a);
