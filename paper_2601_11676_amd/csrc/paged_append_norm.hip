@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_piece(T *p, const C (&x)[kElems<T>])
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (sizeof(T) == 2)
-            v[i] = (uint32_t)f32_to_bf16((float)x[2 * i]) | ((uint32_t)f32_to_bf16((float)x[2 * i + 1]) << 16);
+            v[i] = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)(float)x[2 * i], (__bf16)(float)x[2 * i + 1]});      // one instruction, to nearest even
         else
             v[i] = __float_as_uint((float)x[i]);
     }
@@ -322,16 +322,18 @@ struct ReadArgs {
     void *k_out, *v_out;
     PagePool pool;
     int D, max_pages, n_seq, first;
+    int lanes_log;                                   // 2^lanes_log neighbouring lanes have a row
 };
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void read_q8_kernel(ReadArgs a)
 {
     constexpr int E = kElems<T>;
-    const int token = a.first + blockIdx.x, unit = blockIdx.y * kThreads + threadIdx.x, row_units = a.D / E, units = a.pool.n_kv * row_units;
-    if (unit >= 2 * units) return;
-    const bool value = unit >= units;
-    const int u = value ? unit - units : unit, head = u / row_units, e = (u - head * row_units) * E;
+    const int token = a.first + blockIdx.x, row = (threadIdx.x >> a.lanes_log) + blockIdx.y * (kThreads >> a.lanes_log);
+    const int e = (threadIdx.x & ((1 << a.lanes_log) - 1)) * E;
+    if (row >= 2 * a.pool.n_kv || e >= a.D) return;
+    const bool value = row >= a.pool.n_kv;
+    const int head = value ? row - a.pool.n_kv : row;
     const int seq = a.seq ? a.seq[token] : token, pos = a.pos[token];
     int page = -1;
     if ((unsigned)seq < (unsigned)a.n_seq && (unsigned)pos < (unsigned)(a.max_pages << a.pool.page_shift))
@@ -452,11 +454,12 @@ extern "C" int halo_paged_read_q8(const halo_paged_shape *shape, int32_t N, cons
     a.pos = pos; a.seq = seq; a.table = page_table; a.k_out = k_out; a.v_out = v_out;
     a.pool = PagePool{s.n_pages, s.n_kv_heads, __builtin_ctz((unsigned)s.page_size)};
     a.D = s.head_dim; a.max_pages = s.max_pages; a.n_seq = n_seq;
-    const int units = 2 * s.n_kv_heads * s.head_dim / (s.dtype == HALO_F32 ? 4 : 8);
+    while ((1 << a.lanes_log) * (s.dtype == HALO_F32 ? 4 : 8) < s.head_dim) ++a.lanes_log;
+    const int at_once = kThreads >> a.lanes_log;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     for (int64_t first = 0; first < N; first += kRun) {
         a.first = (int)first;
-        const dim3 grid((unsigned)std::min(kRun, N - first), (units + kThreads - 1) / kThreads), threads(kThreads);
+        const dim3 grid((unsigned)std::min(kRun, N - first), (2 * s.n_kv_heads + at_once - 1) / at_once), threads(kThreads);
         if (s.dtype == HALO_F32) read_q8_kernel<float><<<grid, threads, 0, st>>>(a);
         else read_q8_kernel<bf16_t><<<grid, threads, 0, st>>>(a);
     }

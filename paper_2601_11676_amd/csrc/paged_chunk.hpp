@@ -314,8 +314,7 @@ struct Survivors {
 __device__ __forceinline__ void store_four(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void store_four(bf16_t *p, const float (&v)[4])
 {
-    *reinterpret_cast<uint2 *>(p) = make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
-                                               (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
 }
 
 // A workgroup of WR * WK waves takes 32 WR rows of a cache head's queries; tiles of TT tokens, of which each of the WK waves of the same rows has
