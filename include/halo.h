@@ -484,14 +484,14 @@ int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void
  * drafted tokens to be looked over.  Rows starts[s] .. starts[s+1]-1 of q are the last tokens of sequence s, in order, and lens[s] counts its positions with them: the i-th of
  * its n rows has position p = lens[s] - n + i and
  *   out[row][h] = sum_j p_j V_j,   p = softmax_j(scale * q[row][h] . K_j),   j over positions 0 .. p
- * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it).
+ * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it), nor on other rows.  One to three launches.
  *   q [N][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [N][n_heads][head_dim] dense
  *   starts [n_seq + 1], non-decreasing, lens [n_seq], page_table [n_seq][max_pages] int32 on the device.  Rows before starts[0] and from starts[n_seq] on are
  *       left as they are; a sequence may have none.  Rows outside 0 .. N-1 do not exist.
  *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
  *   mask [N][n_heads] uint8: a head whose byte is 0 gives out = 0; NULL = all survive.
  * Positions in pages that are no pages count as absent; a row without positions (also: more rows than positions) gives out = 0; scores that are all -infinity give NaN.
- * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16; float queries, keys, values and probabilities
+ * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16 (by 2^-8 of each at most; halo_paged_attention keeps all their bits); float queries, keys, values and probabilities
  * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (in keys and queries, floats from 2^128 (1 - 2^-9) on
  * count as infinite, and an infinite one gives NaN).
  * _q8: over a cache of codes, as halo_paged_attention_q8.

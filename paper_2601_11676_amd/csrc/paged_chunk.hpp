@@ -30,7 +30,7 @@ struct ChunkArgs {
 namespace {
 
 constexpr int kCol = 32;                             // columns of the matrix instruction: rows of a block, that is queries
-constexpr int kLeast = 2;                            // tiles of a part at least
+constexpr int kLeast = 2;                            // tiles of a part at least: a part of one is mostly its beginning (some 8 us until the first product)
 constexpr int kDies = 8;
 // Parts that few blocks of so many rows are cut into, about: what is resident at once.
 constexpr int cuts(int rows) { return rows > kCol ? 256 : 512; }
@@ -47,7 +47,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // with i + j < 3 are taken, what is left out is 2^-24 of a product.  kP: of a probability.
 struct KindBf16 {
     typedef bf16_t Row, Cell;                        // queries and results; the cache
-    static constexpr int kQ = 1, kC = 1, kP = 1;
+    static constexpr int kQ = 1, kC = 1, kP = 1;     // of a probability one part: paged_chunk.hip has what two cost
     static constexpr bool kScaled = false, kCheckAll = false;
 };
 struct KindF32 {
