@@ -396,6 +396,19 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     if (a.mask && !a.kept && !__syncthreads_or(kept && row < rows)) tiles = 0;
     const int from = same((int)((int64_t)tiles * line.part / line.parts)), to = same((int)((int64_t)tiles * (line.part + 1) / line.parts));
 
+    // queries are asked for first, so that they travel while the pages' numbers do
+    u32x4 qf[Kind::kQ][QS];
+    {
+        const Row *q = static_cast<const Row *>(a.q) + at * a.q_stride + head * D;
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            const int dim = s * 16 + h * 8;
+            u32x4 p[Kind::kQ];
+            query_parts(q + (EXACT || dim < D ? dim : 0), p);
+#pragma unroll
+            for (int i = 0; i < Kind::kQ; ++i) qf[i][s] = EXACT || dim < D ? p[i] : u32x4{0u, 0u, 0u, 0u};
+        }
+    }
     // page numbers of the parts of 16 tokens, 64 parts at a time, a lane each (-1: no page), and which are pages
     const int32_t *table = a.table + (int64_t)sq * a.max_pages;
     int held = from * L::kParts16, id = 0, id_next = 0;
@@ -428,18 +441,6 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
         pages_next = __ballot(id_next >= 0);
     };
 
-    u32x4 qf[Kind::kQ][QS];
-    {
-        const Row *q = static_cast<const Row *>(a.q) + at * a.q_stride + head * D;
-#pragma unroll
-        for (int s = 0; s < QS; ++s) {
-            const int dim = s * 16 + h * 8;
-            u32x4 p[Kind::kQ];
-            query_parts(q + (EXACT || dim < D ? dim : 0), p);
-#pragma unroll
-            for (int i = 0; i < Kind::kQ; ++i) qf[i][s] = EXACT || dim < D ? p[i] : u32x4{0u, 0u, 0u, 0u};
-        }
-    }
     f32x16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -812,16 +813,18 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
     }
     const int sq = line.find(a, n, lane);
     const Survivors survivors(a, line.seq, sq, kv);
-    const int row0 = line.block * kRows, count = min(survivors.rows - row0, kRows), quads = a.D / 4;
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < count * quads; i += gridDim.y * 256) {
-        const int r = i / quads, q = i - r * quads;
+    // a row is 2^lanes_log neighbouring lanes
+    const int row0 = line.block * kRows, count = min(survivors.rows - row0, kRows), quads = a.D / 4, lanes_log = quads > 32 ? 6 : quads > 16 ? 5 : 4;
+    const int q = threadIdx.x & ((1 << lanes_log) - 1), at_once = 256 >> lanes_log;
+    if (q >= quads) return;
+    for (int r = blockIdx.y * at_once + (threadIdx.x >> lanes_log); r < count; r += gridDim.y * at_once) {
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        // no part past the slots, were starts to go back
+        const int parts = min(line.parts, (a.most - kv + a.pool.n_kv - 1) / a.pool.n_kv - n);
 #pragma unroll 4
-        for (int p = 0; p < line.parts; ++p) {
-            const int64_t place = (int64_t)(n + p) * a.pool.n_kv + kv;
-            if (place >= a.most) break;
-            const int64_t slot = place * kRows + r;
+        for (int p = 0; p < parts; ++p) {
+            const int64_t slot = ((int64_t)(n + p) * a.pool.n_kv + kv) * kRows + r;
             const float2 ml = *reinterpret_cast<const float2 *>(a.stats + slot * 2);
             const float4 v = *reinterpret_cast<const float4 *>(a.part + slot * a.D + q * 4);
             const float next = fmaxf(m, ml.x), use = next == -INFINITY ? 0.0f : next;
