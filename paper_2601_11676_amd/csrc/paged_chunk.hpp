@@ -32,10 +32,7 @@ namespace {
 constexpr int kCol = 32;                             // columns of the matrix instruction: rows of a block, that is queries
 constexpr int kLeast = 2;                            // tiles of a part at least: a part of one is mostly its beginning (some 8 us until the first product)
 constexpr int kDies = 8;
-// Parts that few blocks of so many rows are cut into, about: what is resident at once.
-constexpr int cuts(int rows) { return rows > kCol ? 256 : 512; }
-constexpr int kPartRows = 2 * 256 * 8 * kCol;        // rows of partial results: a part for each cut and one more for each block, fewer than cuts
-static_assert(2 * cuts(kCol) * kCol <= kPartRows, "of narrow blocks too");
+constexpr int kPartRows = 2 * 256 * 8 * kCol;        // rows of partial results: see Layout::kCuts
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -201,7 +198,7 @@ __device__ __forceinline__ Sequence sequence(const ChunkArgs &a, int s)
 
 // The line of all parts of all blocks of rows of one cache head: sequence by sequence, long ones first (up to 64 of them; of more in their order), and a sequence's blocks that see
 // the most first, so that what begins last is short.  All of a wave-uniform; a lane has a sequence.
-template <int kRows, int kTile>
+template <int kRows, int kTile, int kCuts>
 struct Line {
     int per, items;                                  // tiles of a part at most (0: nothing is cut); parts of a cache head
     Sequence own;                                    // up to 64 sequences: of the lane's, in the line's order; its number and the parts up to its end
@@ -236,7 +233,7 @@ struct Line {
             }
             tiles = wave_sum(tiles) * a.pool.n_kv;
             blocks = wave_sum(blocks) * a.pool.n_kv;
-            per = same(max((int)fminf(tiles / fmaxf(cuts(kRows) - 0.5f * blocks, 0.25f * cuts(kRows)), 1e9f) + 1, kLeast));
+            per = same(max((int)fminf(tiles / fmaxf(kCuts - 0.5f * blocks, 0.25f * kCuts), 1e9f) + 1, kLeast));
         }
         if (few) {
             end = upto(own.blocks(a.group, kRows) * own.parts(kTile, per));
@@ -331,6 +328,9 @@ struct Layout {
     static constexpr int kRowBytes = DP * (int)sizeof(Cell), kRowLanes = kRowBytes / 16, kRowsEach = 64 / kRowLanes, kLoads = TT / kRowsEach;
     static constexpr int kEach = (kLoads + kWaves - 1) / kWaves, kParts16 = TT / 16, kPerPart = kEach * kRowsEach > 16 ? 16 / kRowsEach : kEach;
     static_assert(16 % kRowsEach == 0 && (kLoads % kWaves == 0 || kLoads < kWaves), "whole loads");
+    // Waves of a SIMD (two for float heads of 64 too: 4 sequences of 4000 in all, 32 heads, 147 us with one, 137); and the parts that few blocks are cut into, about: what is resident at once.  Their partial results are of a part each and one more for each block, fewer than parts.
+    static constexpr int kOnSimd = DP * Kind::kC <= 192 ? 2 : 1, kCuts = kOnSimd * 4 > kWaves ? 512 : 256;
+    static_assert(2 * kCuts * kRows <= kPartRows, "partial results in the workspace");
 };
 
 // Where a lane's 16 bytes lie in LDS: key rows are read 16 bytes a lane, a row a lane; value rows 16 dimensions of four rows at a time.  The pieces of a row change
@@ -361,7 +361,7 @@ __device__ __forceinline__ void reads_ahead()
 }
 
 template <typename Kind, int DP, bool EXACT, int WR, int WK>
-__global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void chunk_attend(ChunkArgs a)
+__global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) void chunk_attend(ChunkArgs a)
 {
     typedef Layout<Kind, DP, WR, WK> L;
     typedef typename Kind::Row Row;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
     const int c = lane & 31, h = lane >> 5;
     const int D = EXACT ? DP : a.D;
 
-    Line<L::kRows, TT> line(a, lane);
+    Line<L::kRows, TT, L::kCuts> line(a, lane);
     int item, kv;
     if (!place_of(a, blockIdx.x, line.items, item, kv)) return;
     const int sq = line.find(a, item, lane);
@@ -785,11 +785,11 @@ __global__ __launch_bounds__(WR * WK * 64, DP * Kind::kC <= 128 ? 2 : 1) void ch
 }
 
 // Joins the blocks that were cut.  Workgroups stand for blocks of rows (x), cut by y; a thread stands for four dimensions of a row.
-template <typename Row, int kRows, int kTile>
+template <typename Row, int kRows, int kTile, int kCuts>
 __global__ __launch_bounds__(256) void chunk_join(ChunkArgs a)
 {
     const int lane = threadIdx.x & 63, kv = blockIdx.z;
-    Line<kRows, kTile> line(a, lane);
+    Line<kRows, kTile, kCuts> line(a, lane);
     // the x-th of those that are cut: the first part of each block is its place in the line
     int n = 0;
     {
@@ -917,9 +917,9 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     // of a cache head at most: for a call whose starts go back, what is beyond is left out
     const int64_t heads = a.pool.n_kv, blocks = most_blocks(a, L::kRows);
     int64_t grid = blocks;
-    const bool cut = blocks < cuts(L::kRows) && a.max_len > kLeast * L::TT;
+    const bool cut = blocks < L::kCuts && a.max_len > kLeast * L::TT;
     if (cut) {
-        grid += cuts(L::kRows);                              // a part more than even shares give, for each block
+        grid += L::kCuts;                              // a part more than even shares give, for each block
         a.slots = (int)grid;
     }
     a.most = (int)grid;
@@ -938,7 +938,7 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     chunk_attend<Kind, DP, EXACT, WR, WK><<<dim3((unsigned)grid), dim3(L::kThreads), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return HALO_ERR_HIP;
     if (!cut) return HALO_OK;
-    chunk_join<typename Kind::Row, L::kRows, L::TT><<<dim3((unsigned)(blocks / heads), (L::kRows * (a.D / 4) + 511) / 512, (unsigned)heads), dim3(256), 0, s>>>(a);
+    chunk_join<typename Kind::Row, L::kRows, L::TT, L::kCuts><<<dim3((unsigned)(blocks / heads), (L::kRows * (a.D / 4) + 511) / 512, (unsigned)heads), dim3(256), 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? HALO_OK : HALO_ERR_HIP;
 }
 
