@@ -1,5 +1,9 @@
 """Chunks over a paged cache, a cache of codes and appends that norm, without a GPU: what the entry points refuse, calls that do nothing, the workspace, what is launched."""
 import ctypes as C
+import json
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -7,6 +11,7 @@ import torch
 import paper_2601_11676_amd as H
 from paper_2601_11676_amd.binding import _pool_q8
 
+HERE = os.path.dirname(os.path.abspath(__file__))
 ONE, ODD, OFF, NULL, ST = C.c_void_p(0x1000), C.c_void_p(0x1004), C.c_void_p(0x1002), None, C.c_void_p(0)     # never dereferenced
 
 
@@ -128,3 +133,68 @@ def test_binding_refuses_what_the_library_cannot_see():
         _pool_q8((c.float(), pool[1]), s)
     with pytest.raises(ValueError, match="row of the page table"):
         H.halo_paged_read_q8(s, i, torch.zeros(2, 4, dtype=torch.int32), pool, pool, x, x)
+
+
+# ---------------------------------------------------------------- what is launched
+CALLS = """
+import ctypes as C, json, sys
+recorder = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+recorder.recorder_take.restype = C.c_char_p
+lib = C.CDLL(sys.argv[2])
+lib.halo_paged_chunk_workspace_bytes.restype = C.c_size_t
+p, i64, out = C.c_void_p(1 << 30), C.c_int64, []
+for what, heads, kv, dim, dtype, N, n_seq, max_len, mask in json.load(sys.stdin):
+    shape = C.byref((C.c_int32 * 7)(heads, kv, dim, 16, 1000, max(1, (max_len + 15) // 16), dtype))
+    if what == "read":
+        rc = lib.halo_paged_read_q8(shape, N, p, p, n_seq, p, p, p, p, p, p, p, None)
+    elif what == "codes":
+        rc = lib.halo_paged_append_q8(shape, N, p, i64(heads * dim), p, i64(kv * dim), p, i64(kv * dim), p, p, n_seq, p, 1, p, p, C.c_float(1e-5), None, 0, 0, 0,
+                                      C.c_void_p(1 << 31), p, p, p, p, None)
+    else:
+        ws = i64(lib.halo_paged_chunk_workspace_bytes(shape, N, n_seq))
+        pools = [p] * (4 if what == "q8" else 2)
+        fn = lib.halo_paged_chunk_attention_q8 if what == "q8" else lib.halo_paged_chunk_attention
+        rc = fn(shape, N, p, i64(heads * dim), *pools, n_seq, p, p, p, max_len, p if mask else None, C.c_float(1.0), p, p, ws, None)
+    out.append((rc, [l.split() for l in recorder.recorder_take().decode().split("\\n")[:-1]]))
+json.dump(out, sys.stdout)
+"""
+
+
+def _launches(calls, tmp_path):
+    shim = str(tmp_path / "recorder.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", shim, os.path.join(HERE, "launch_recorder.c")], check=True)
+    p = subprocess.run([sys.executable, "-c", CALLS, shim, H.library_path()], input=json.dumps(calls), capture_output=True, text=True, timeout=120)
+    assert p.returncode == 0, p.stderr
+    return json.loads(p.stdout)
+
+
+def test_chunk_launches(tmp_path):
+    # (cache, heads, cache heads, dim, dtype, tokens, sequences, longest, mask) -> kernels, rows of a block, workgroups of the first that attends
+    up = lambda n: -(-n // 8) * 8
+    cases = [(("rows", 64, 8, 128, 1, 512, 1, 16512, 0), ["chunk_attend", "chunk_join"], up(17 * 8 + 256)),              # few blocks: cut
+             (("rows", 40, 40, 128, 1, 4099, 7, 937, 1), ["chunk_attend"], 920),                                         # many: whole
+             (("rows", 32, 32, 128, 1, 8192, 1, 8192, 1), ["chunk_rows", "chunk_attend"], up(33 * 32)),                  # many scores under a mask
+             (("rows", 64, 8, 128, 1, 640, 16, 3040, 0), ["chunk_attend"], up((640 * 8 // 128 + 16) * 8)),               # blocks of 128 rows
+             (("q8", 64, 8, 128, 1, 4, 4, 3000, 0), ["chunk_attend", "chunk_join"], up(5 * 8 + 512)),                    # of 32
+             (("q8", 64, 8, 128, 1, 4, 4, 256, 0), ["chunk_attend"], up(5 * 8)),                                         # a part has two tiles at least
+             (("rows", 12, 4, 64, 0, 777, 3, 545, 0), ["chunk_attend", "chunk_join"], up((777 * 3 // 128 + 3) * 4 + 512)),
+             (("q8", 8, 8, 64, 0, 0, 3, 64, 0), [], 0)]
+    for (call, names, groups), (rc, got) in zip(cases, _launches([c for c, _, _ in cases], tmp_path)):
+        assert rc == 0 and len(got) == len(names), (call, got)
+        assert all(n in g[0] for n, g in zip(names, got)), (call, got)
+        attend = [g for g in got if "chunk_attend" in g[0]]
+        assert not attend or int(attend[0][1]) == groups, (call, got)
+
+
+def test_grids_of_any_call_stay_within_a_launch(tmp_path):
+    calls = [(what, heads, kv, dim, dtype, N, n_seq, max_len, mask)
+             for heads, kv in ((256, 1), (256, 256), (1, 1), (64, 8)) for dim, dtype in ((128, 1), (64, 0), (256, 0), (16, 1))
+             for N, n_seq, max_len in ((1, 1, 1 << 30), (1 << 21, 1, 1 << 30), (1 << 21, 4096, 1 << 20), (4096, 4096, 5), (5, 4096, 1 << 20))
+             for what, mask in (("rows", 0), ("rows", 1), ("q8", 1))]
+    calls += [(what, 8, 8, dim, 1, N, 9, 64, 0) for what in ("read", "codes") for dim in (16, 256) for N in (1, 1 << 24, (1 << 31) - 1)]
+    for call, (rc, launches) in zip(calls, _launches(calls, tmp_path)):
+        assert rc == 0 and launches, call
+        for _, x, y, z, threads in launches:
+            assert 0 < int(x) * int(threads) < 1 << 32 and 0 < int(y) <= 65535 and 0 < int(z) <= 65535, (call, launches)
+        if call[0] in ("read", "codes"):
+            assert sum(int(g[1]) for g in launches) == call[5]
