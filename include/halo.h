@@ -462,7 +462,8 @@ int halo_paged_append_norm(const halo_paged_shape *shape, int32_t N, const void 
  * pointers), HALO_ERR_HIP.
  *
  * halo_paged_attention_q8: halo_paged_attention over such a cache (with halo_paged_workspace_bytes).  Products are of the codes themselves, a key's scale multiplies its score, a
- * value's its probability; float queries and all probabilities enter the products as three bf16 values, which hold all of their bits.
+ * value's its probability; float queries and all probabilities enter the products as three bf16 values, which hold all of their bits (of
+ * numbers from 2^-110 on: parts below 2^-126 count as 0).
  */
 int halo_paged_append_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                          const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
@@ -484,7 +485,7 @@ int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void
  * drafted tokens to be looked over.  Rows starts[s] .. starts[s+1]-1 of q are the last tokens of sequence s, in order, and lens[s] counts its positions with them: the i-th of
  * its n rows has position p = lens[s] - n + i and
  *   out[row][h] = sum_j p_j V_j,   p = softmax_j(scale * q[row][h] . K_j),   j over positions 0 .. p
- * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it), nor on other rows.  One to three launches.
+ * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it), nor on what other rows hold.  One to three launches.
  *   q [N][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [N][n_heads][head_dim] dense
  *   starts [n_seq + 1], non-decreasing, lens [n_seq], page_table [n_seq][max_pages] int32 on the device.  Rows before starts[0] and from starts[n_seq] on are
  *       left as they are; a sequence may have none.  Rows outside 0 .. N-1 do not exist.
@@ -492,8 +493,9 @@ int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void
  *   mask [N][n_heads] uint8: a head whose byte is 0 gives out = 0; NULL = all survive.
  * Positions in pages that are no pages count as absent; a row without positions (also: more rows than positions) gives out = 0; scores that are all -infinity give NaN.
  * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16 (by 2^-8 of each at most; halo_paged_attention keeps all their bits); float queries, keys, values and probabilities
- * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (in keys and queries, floats from 2^128 (1 - 2^-9) on
- * count as infinite, and an infinite one gives NaN).
+ * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (an infinite
+ * float key or query gives NaN).  Sums of values hold up to 2^8 times their weights until they are divided: values of 2^120 and more may overflow.
+ * Parts below 2^-126 count as 0: floats below 2^-110 enter with fewer bits.
  * _q8: over a cache of codes, as halo_paged_attention_q8.
  * How the work is cut depends on the arguments that the host sees and on the lengths; results do not depend on timing.
  * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N outside 0..2^21, n_seq outside 0..4096, max_len, stride, alignment, scale not

@@ -65,7 +65,8 @@ struct KindQ8F32 {
     static constexpr bool kScaled = true, kCheckAll = false;
 };
 
-constexpr float kLargest = 0x1.fep127f;              // floats below it are finite as bf16
+// The largest bf16 number: a first part goes no further, so that floats beyond it do not become infinite (what is left of one has 16 bits).
+__device__ __forceinline__ float first_part(float v) { return __builtin_amdgcn_fmed3f(v, -0x1.fep127f, 0x1.fep127f); }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
@@ -82,7 +83,7 @@ __device__ __forceinline__ void parts_of(const float (&x)[8], u32x4 (&out)[P])
         float a = x[2 * i], b = x[2 * i + 1];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            out[p][i] = pack_bf16(a, b);
+            out[p][i] = P > 1 && p == 0 ? pack_bf16(first_part(a), first_part(b)) : pack_bf16(a, b);
             if (p + 1 < P) {
                 a -= bf16_lo(out[p][i]);
                 b -= bf16_hi(out[p][i]);
@@ -124,7 +125,7 @@ template <> struct Piece<float> {
             float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                out[p][i] = pack_bf16(a, b);
+                out[p][i] = p == 0 ? pack_bf16(first_part(a), first_part(b)) : pack_bf16(a, b);
                 a -= bf16_lo(out[p][i]);
                 b -= bf16_hi(out[p][i]);
             }
@@ -135,8 +136,7 @@ template <> struct Piece<float> {
         bool any = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            // the largest floats, which round to infinity as bf16, count with the infinities: they are added as they are too
-            const bool x = !(fabsf(__uint_as_float(v[i])) < kLargest);
+            const bool x = !(fabsf(__uint_as_float(v[i])) < INFINITY);
             any = any || x;
             v[i] = x ? 0u : v[i];
         }
@@ -691,7 +691,7 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
                         for (int i = 0; i < 16; ++i) {
                             const int dim = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
                             const float w = EXACT || dim < D ? to_float(v[dim]) : 0.0f;
-                            if (!(fabsf(w) < (Kind::kC > 1 ? kLargest : INFINITY)) && pos < lim) acc[d][i] += w;
+                            if (!(fabsf(w) < INFINITY) && pos < lim) acc[d][i] += w;
                         }
                 }
         }

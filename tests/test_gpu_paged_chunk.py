@@ -275,6 +275,25 @@ def test_scores_of_infinity(kind):
     assert torch.all((got[1, 0].double() - case.v[page[0], 0, 1].double()).abs() <= one)
 
 
+def test_large_and_small_floats_are_numbers():
+    # A value that a row sees alone is its result, to the bit: probability 1, three parts that add up; up to 2^120, from where sums may overflow on their way (the largest float is
+    # (2^8 - 1) 2^120 + 2^120 - 2^104 in parts, whose first two are 2^128), and from 2^-110 on, below which last parts are below 2^-126 and count as 0.  A key past the largest bf16 number against a query of 2^-126: the product is a number like any other.
+    largest = torch.finfo(torch.float32).max
+    case = Case("f32", 4, 2, 64, 16, [(0, 1)] * 6 + [(0, 2)], seed=17)
+    for i, v in enumerate([largest * 2.0 ** -8, -largest * 2.0 ** -8, 1.3e36, -1.2345678e36, 3.3895e35, 1.2345678e-32]):
+        case.v[int(case.table[i, 0]), :, 0, i::7] = v
+    case.q = case.q.clone()
+    case.q[6:, :, 9] = 2.0 ** -126
+    page = int(case.table[6, 0])
+    case.k[page, :, 1, 9], case.k[page, :, 0, 9] = largest, 0.0
+    got = case.run()
+    for i in range(6):
+        assert torch.equal(got[i], case.v[int(case.table[i, 0]), :, 0].repeat_interleave(2, 0))
+    # scores of at most 8 * 8 / 8 + 4 / 8 with 65 terms, each product and sum of six passes off by 2^-24 of it: 6 * 65 * 9 * 2^-24 = 2.1e-4, twice in a probability, of values up to 5
+    want, _ = case.want()
+    assert torch.all((got[6:].double() - want[6:]).abs() <= 2 * 2.1e-4 * 2 * 5)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_nan_stays_in_its_row(kind):
     case = Case(kind, 4, 2, 128, 16, [(50, 60)], seed=8)
