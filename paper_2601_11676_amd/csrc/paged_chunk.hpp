@@ -329,7 +329,7 @@ struct Layout {
     static constexpr int kEach = (kLoads + kWaves - 1) / kWaves, kParts16 = TT / 16, kPerPart = kEach * kRowsEach > 16 ? 16 / kRowsEach : kEach;
     static_assert(16 % kRowsEach == 0 && (kLoads % kWaves == 0 || kLoads < kWaves), "whole loads");
     // Waves of a SIMD (two for float heads of 64 too: 4 sequences of 4000 in all, 32 heads, 147 us with one, 137); and the parts that few blocks are cut into, about: what is resident at once.  Their partial results are of a part each and one more for each block, fewer than parts.
-    static constexpr int kOnSimd = DP * Kind::kC <= 192 ? 2 : 1, kCuts = kOnSimd * 4 > kWaves ? 512 : 256;
+    static constexpr int kOnSimd = DP * Kind::kC <= 192 && kLds * (8 / kWaves) <= 163840 ? 2 : 1, kCuts = kOnSimd * 4 > kWaves ? 512 : 256;
     static_assert(2 * kCuts * kRows <= kPartRows, "partial results in the workspace");
 };
 
@@ -700,31 +700,29 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
     if (tid < L::kBufs) s_bad[tid] = 0;
     if (from < to) fetch(from);
     __syncthreads();
-    {
-        auto step = [&](int t, int buf) {
-            scores(t, buf);
-            soften(t, buf);
-            product(t, buf);
-        };
-        if constexpr (L::kBufs == 2) {
-            if (from < to) put(from, 0);
-            for (int t = from; t < to; ++t) {
-                const int buf = (t - from) & 1;
-                __syncthreads();
-                advance(t * L::kParts16);
-                fetch(t + 1);
-                if (t * TT < most) step(t, buf);
-                put(t + 1, buf ^ 1);
-            }
-        } else {
-            for (int t = from; t < to; ++t) {
-                put(t, 0);
-                __syncthreads();
-                advance(t * L::kParts16);
-                fetch(t + 1);
-                if (t * TT < most) step(t, 0);
-                __syncthreads();
-            }
+    auto step = [&](int t, int buf) {
+        scores(t, buf);
+        soften(t, buf);
+        product(t, buf);
+    };
+    if constexpr (L::kBufs == 2) {
+        if (from < to) put(from, 0);
+        for (int t = from; t < to; ++t) {
+            const int buf = (t - from) & 1;
+            __syncthreads();
+            advance(t * L::kParts16);
+            fetch(t + 1);
+            if (t * TT < most) step(t, buf);
+            put(t + 1, buf ^ 1);                     // which every wave was done with before the barrier
+        }
+    } else {
+        for (int t = from; t < to; ++t) {
+            put(t, 0);
+            __syncthreads();
+            advance(t * L::kParts16);
+            fetch(t + 1);
+            if (t * TT < most) step(t, 0);
+            __syncthreads();
         }
     }
     l = xor_add<32>(l);
