@@ -472,11 +472,11 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
             for (int i = 0; i < L::kPerPart; ++i) vp[j + i].v = buffer_load16<0>(v_rows, voff + i * L::kRowsEach * D * kRow, 0);
         }
         if constexpr (Kind::kScaled) {
-            if (tid < TT) {
+            if (wave * 64 < TT) {                    // whole waves, of tiles of 32 too: an exchange takes nothing from lanes that are not there
                 const int pos = t * TT + tid, part = t * L::kParts16 + tid / 16 - held;
                 const int p0 = __shfl(id, part & 63), p1 = __shfl(id_next, part & 63);
                 const int page = part < 64 ? p0 : p1;
-                const bool in = page >= 0 && pos < block_most && t < to;
+                const bool in = tid < TT && page >= 0 && pos < block_most && t < to;
                 const int64_t r = in ? paged_row(a.pool, page, kv, pos) : 0;
                 kps = in ? a.k_scale[r] * a.scale2 : 0.0f;
                 vps = in ? a.v_scale[r] : 0.0f;
