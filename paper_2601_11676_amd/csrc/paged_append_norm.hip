@@ -190,7 +190,8 @@ struct HeadRow {
         }
     }
     // As codes.  A product with 127 / max says which, unless it lies so near the border of two that its error decides: within 2e-5 in float (two roundings of a number
-    // up to 127, 127 * 2^-23) and 1e-6 in double.  A lane that has one of those takes exact quotients.
+    // up to 127, 127 * 2^-23) and 1e-6 in double.  A lane that has one of those takes quotients 127 x / max, rounded once: of rows that came as floats 127 x is exact, and of such
+    // numbers no quotient that is no tie lies within 2^-35 of one, so that ties, and they alone, go to even.
     __device__ __forceinline__ void store_codes(int8_t *row, float *scale, int lanes, int e0, int e1, bool in, bool first) const
     {
         C top = (C)0, odd = (C)0;                    // 0 times an infinity or NaN is NaN
@@ -220,10 +221,9 @@ struct HeadRow {
 #pragma unroll
             for (int i = 0; i < E / 4; ++i) w[0][i] = w[1][i] = 0;
         } else if ((far > border || few) && top > (C)0) {
-            const double exact = (double)top / 127.0;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const uint32_t u = (uint32_t)(uint8_t)(int)rint((double)x[i] / exact), v = (uint32_t)(uint8_t)(int)rint((double)y[i] / exact);
+                const uint32_t u = (uint32_t)(uint8_t)(int)rint(127.0 * x[i] / (double)top), v = (uint32_t)(uint8_t)(int)rint(127.0 * y[i] / (double)top);
                 w[0][i / 4] = i % 4 ? w[0][i / 4] | u << (8 * (i % 4)) : u;
                 w[1][i / 4] = i % 4 ? w[1][i / 4] | v << (8 * (i % 4)) : v;
             }
