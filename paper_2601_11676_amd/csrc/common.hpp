@@ -12,6 +12,9 @@ constexpr int kWave = 64;
 
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+// Of a float that goes to the matrix cores as several bf16 parts, the first before its rounding: no further than the largest bf16 number, so that floats beyond it do not become
+// infinite (what is left of one has 16 bits).
+__device__ __forceinline__ float first_part(float v) { return __builtin_amdgcn_fmed3f(v, -0x1.fep127f, 0x1.fep127f); }
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }

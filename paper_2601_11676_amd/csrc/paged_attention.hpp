@@ -559,7 +559,7 @@ struct CoreQ8 {
                     float a = in ? x[2 * i] : 0.0f, b = in ? x[2 * i + 1] : 0.0f;
 #pragma unroll
                     for (int p = 0; p < QP; ++p) {
-                        qf[t][p][s][i] = pair(a, b);
+                        qf[t][p][s][i] = QP > 1 && p == 0 ? pair(first_part(a), first_part(b)) : pair(a, b);
                         a -= bf16_lo(qf[t][p][s][i]);
                         b -= bf16_hi(qf[t][p][s][i]);
                     }

@@ -65,9 +65,6 @@ struct KindQ8F32 {
     static constexpr bool kScaled = true, kCheckAll = false;
 };
 
-// The largest bf16 number: a first part goes no further, so that floats beyond it do not become infinite (what is left of one has 16 bits).
-__device__ __forceinline__ float first_part(float v) { return __builtin_amdgcn_fmed3f(v, -0x1.fep127f, 0x1.fep127f); }
-
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

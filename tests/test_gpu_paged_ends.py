@@ -1,8 +1,9 @@
-"""The paged operators where a definition decides a single bit: codes of exact ties."""
+"""The paged operators where a definition decides a single bit: codes of exact ties, float queries that round past the largest bf16 number."""
 import pytest
 import torch
 
-from tests.test_gpu_paged_q8 import Append
+import paper_2601_11676_amd as H
+from tests.test_gpu_paged_q8 import DEV, Append
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,32 @@ def test_ties_of_ordinary_rows_go_to_even(dtype, coarse):
         ties += int((quotient - torch.floor(quotient) == 0.5).sum())
         assert torch.equal(codes.cpu()[page, :, row].double(), torch.round(quotient))
     assert not coarse or ties > 500                                   # of 614400
+
+
+def test_float_queries_past_the_largest_bf16_number_over_codes():
+    # Rounded to one bf16 number such a query would be an infinity, and with a code of 0 NaN.  Head 0: the largest float, codes of 0 there, the rest as it is; head 1: 255.7 * 2^120 (of
+    # more the first two parts may add up to 2^128), codes of 0 and 1 and scales of some 2^-126, which leave scores of up to 2.
+    D, n = 64, 50
+    g = torch.Generator().manual_seed(32)
+    shape = H.PagedShape(2, 2, D, 16, 4, 4, "f32")
+    k, v = (torch.randint(-127, 128, shape.pool, generator=g, dtype=torch.int8) for _ in range(2))
+    ks, vs = (0.005 + 0.02 * torch.rand(shape.pool[:3], generator=g) for _ in range(2))
+    q = torch.randn(1, 2, D, generator=g)
+    q[0, 0, 20], q[0, 1, 20] = torch.finfo(torch.float32).max, 255.7 * 2.0 ** 120
+    k[:, 0, :, 20] = 0
+    k[:, 1, :, 20] = torch.randint(0, 2, (4, 16), generator=g, dtype=torch.int8)
+    ks[:, 1] = (1 + 3 * torch.rand(4, 16, generator=g)) * 2.0 ** -126
+    out = torch.empty(1, 2, D, device=DEV)
+    ws = torch.empty(H.halo_paged_workspace_bytes(shape, 1), dtype=torch.uint8, device=DEV)
+    H.halo_paged_attention_q8(shape, q.to(DEV), (k.to(DEV), ks.to(DEV)), (v.to(DEV), vs.to(DEV)), torch.arange(4, dtype=torch.int32, device=DEV)[None],
+                              torch.tensor([n], dtype=torch.int32, device=DEV), n, out, ws, scale=0.125)
+    out = out.cpu().double()
+    assert torch.isfinite(out).all()
+    kk, vv = ((c.double() * s.double()[..., None]).transpose(0, 1).reshape(2, 64, D)[:, :n] for c, s in ((k, ks), (v, vs)))
+    for h in range(2):
+        x, F = q[0, h].double(), 2.0 ** -24
+        p = torch.softmax(kk[h] @ x * 0.125, 0)
+        # scores off by three passes of D roundings of sum |q k|, scale and exponent by a few, sums of n: as where all queries are ordinary
+        S = 0.125 * float((kk[h].abs() @ x.abs()).max())
+        off = 2 * F * (6 * D * S + 12 * S + 3 * n + 80) * (p @ vv[h].abs())
+        assert torch.all((out[0, h] - p @ vv[h]).abs() <= off + F * (p @ vv[h]).abs())
