@@ -650,6 +650,21 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
     };
     auto product = [&](int t, int buf) {
         const char *const s_v = values_of(buf);
+        // of a tile with values that are no finite numbers: the lane's probabilities that are 0
+        bool bad = false;
+        uint32_t none = 0;
+        if constexpr (!Kind::kScaled) {
+            bad = s_bad[buf] == t + 1;
+            if (bad) {
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t two = pp[n][i / 4][0][i % 4];
+                        none |= (two & 0x7fffu ? 0u : 1u) << (16 * n + 2 * i) | (two & 0x7fff0000u ? 0u : 2u) << (16 * n + 2 * i);
+                    }
+            }
+        }
 #pragma unroll
         for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -674,13 +689,15 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
                 }
             }
         if constexpr (EXACT) reads_ahead<NS * 2 * DB * Kind::kC, products(Kind::kP, Kind::kC) / Kind::kC, 2>();
-        // Values that are no finite numbers were left out of the products (0 * infinity would reach the rows that do not see them): they are added as they
-        // are to the rows that do.
+        // Values that are no finite numbers were left out of the products (0 * infinity would reach the rows that do not see them): the rows that do have them added, as
+        // products with their probabilities: themselves, or NaN where that is 0.
         if constexpr (!Kind::kScaled) {
-            if (s_bad[buf] == t + 1)
+            if (bad)
                 for (int tt = 0; tt < 32 * NS; ++tt) {
                     const int r0 = (tt / 32 * WK + wk) * 32 + tt % 32, pos = t * TT + r0, page = page_of(t * L::kParts16 + r0 / 16);
                     if (page < 0 || pos >= block_most) continue;
+                    const uint32_t bits = (uint32_t)__shfl((int)none, c + (tt & 4) * 8);         // of the lane that has the row's probability of this token
+                    const bool zero = bits >> (tt / 32 * 16 + tt % 32 / 8 * 4 + tt % 4) & 1;
                     const Cell *v = static_cast<const Cell *>(a.v) + paged_row(a.pool, page, kv, pos) * D;
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
@@ -688,7 +705,7 @@ __global__ __launch_bounds__(WR * WK * 64, (Layout<Kind, DP, WR, WK>::kOnSimd)) 
                         for (int i = 0; i < 16; ++i) {
                             const int dim = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
                             const float w = EXACT || dim < D ? to_float(v[dim]) : 0.0f;
-                            if (!(fabsf(w) < INFINITY) && pos < lim) acc[d][i] += w;
+                            if (!(fabsf(w) < INFINITY) && pos < lim) acc[d][i] += zero ? NAN : w;
                         }
                 }
         }

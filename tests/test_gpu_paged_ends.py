@@ -1,8 +1,11 @@
-"""The paged operators where a definition decides a single bit: codes of exact ties, float queries that round past the largest bf16 number."""
+"""The paged operators where a definition decides a single bit: codes of exact ties, float queries that round past the largest bf16 number, infinite values whose probability is 0."""
+import math
+
 import pytest
 import torch
 
 import paper_2601_11676_amd as H
+from tests.test_gpu_paged_chunk import Case
 from tests.test_gpu_paged_q8 import DEV, Append
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +56,41 @@ def test_float_queries_past_the_largest_bf16_number_over_codes():
         S = 0.125 * float((kk[h].abs() @ x.abs()).max())
         off = 2 * F * (6 * D * S + 12 * S + 3 * n + 80) * (p @ vv[h].abs())
         assert torch.all((out[0, h] - p @ vv[h]).abs() <= off + F * (p @ vv[h]).abs())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hk,D,past,new", [(2, 2, 64, 300, 40), (4, 1, 128, 200, 100), (1, 1, 256, 150, 90), (64, 32, 64, 0, 700)])
+@pytest.mark.parametrize("low", [-math.inf, -400.0])
+def test_infinite_values_whose_probability_is_0(kind, Hq, Hk, D, past, new, low):
+    # Elements of 0 * infinity are NaN, whatever the tile: positions that all rows of a block see, and positions among the block's own.  Infinities that count stay infinities, and
+    # rows before such positions keep their bits.  low: the score of those positions (exp of -400 and less is 0 in float); -infinity only of bf16 (infinite float keys give NaN).
+    if low == -math.inf and kind == "f32":
+        low = -3.0e38
+    case = Case(kind, Hq, Hk, D, 16, [(past, new)], seed=33, sigma=0.2)
+    case.q = case.q.clone()
+    case.q[..., 0] = 1.0                                              # scores: what key element 0 has, and little else
+    n, s = past + new, case.shape
+    for j in range(n):
+        case.k[int(case.table[0, j // 16]), :, j % 16, 0] = 0.0
+    clean = case.run()
+    none = sorted({7, past + 9, past + new // 2, n - 5})              # probability 0, of all rows that see them
+    full = [past + 21, n - 3]                                         # ordinary ones
+    for j, (value, dim) in [(j, (math.inf, 3)) for j in none] + [(j, (-math.inf, 5)) for j in full]:
+        page, row = int(case.table[0, j // 16]), j % 16
+        case.v[page, :, row, dim] = value
+        if dim == 3:
+            case.k[page, :, row, 0] = low if math.isinf(low) or low < -1e30 else low / case.scale
+    got = case.run()
+    for i in range(new):
+        pos = past + i
+        seen = [j for j in none if j <= pos]
+        assert torch.isnan(got[i, :, 3]).all() if seen else torch.isfinite(got[i, :, 3]).all(), (i, got[i, :, 3])
+        if any(j <= pos for j in full):
+            assert torch.all(got[i, :, 5] == -math.inf), i
+        else:
+            assert torch.isfinite(got[i, :, 5]).all(), i
+        other = [d for d in range(D) if d not in (3, 5)]
+        assert torch.isfinite(got[i][:, other]).all()
+    first = min(none + full)
+    if first >= past:
+        assert torch.equal(got[:first - past], clean[:first - past])
