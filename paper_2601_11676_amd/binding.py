@@ -466,8 +466,8 @@ def _pool_q8(pool, shape: PagedShape):
     return _dense(codes, torch.int8, shape.pool_elems), _dense(scales, torch.float32, shape.pool_elems // shape.head_dim)
 
 
-def _new_tokens(shape: PagedShape, q, k, v, pos, page_table, q_out, seq):
-    """What all appends take of their tokens: the arguments from N to page_table, and q_out's address."""
+def _append(name, shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out, rope, rope_pairs, seq, stream, norm=None, codes=False):
+    """All appends.  norm: what stands for it in the call (None: an append that has none); codes: the pages are pairs (codes, scales)."""
     dt, dim, n_kv = shape.torch_dtype, shape.head_dim, shape.n_kv_heads
     pk, sk, N = _heads(k, n_kv, dim, dt)
     pv, sv, Nv = _heads(v, n_kv, dim, dt)
@@ -481,53 +481,52 @@ def _new_tokens(shape: PagedShape, q, k, v, pos, page_table, q_out, seq):
     n_seq = page_table.shape[0]
     if seq is None and n_seq < N:
         raise ValueError("without seq, every token needs a row of the page table")
-    return (N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N), n_seq,
-            _dense(page_table, torch.int32, n_seq * shape.max_pages)), po
+    pr, rows, half = None, 0, 0
+    if rope is not None:
+        rows, _, half = rope.shape
+        if not rows or not half:                     # without an address it would mean no rotation
+            raise ValueError("a table of angles has rows and columns")
+        pr = _dense(rope, torch.float32, rows * 2 * half)
+    if norm is None:                                 # written out: starred arguments cost 0.5 us a call
+        rc = load_library().halo_paged_append(
+            shape.c, N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N),
+            n_seq, _dense(page_table, torch.int32, n_seq * shape.max_pages), pr, rows, 2 * half, 1 if rope_pairs else 0, po,
+            _pool(k_pages, shape), _pool(v_pages, shape), _stream(stream))
+    else:
+        pools = (*_pool_q8(k_pages, shape), *_pool_q8(v_pages, shape)) if codes else (_pool(k_pages, shape), _pool(v_pages, shape))
+        rc = getattr(load_library(), name)(
+            shape.c, N, pq, sq, pk, sk, pv, sv, _dense(pos, torch.int32, N), None if seq is None else _dense(seq, torch.int32, N),
+            n_seq, _dense(page_table, torch.int32, n_seq * shape.max_pages), *norm, pr, rows, 2 * half, 1 if rope_pairs else 0, po, *pools,
+            _stream(stream))
+    if rc:
+        raise HaloError(name, rc)
 
 
-def _angles(rope):
-    if rope is None:
-        return None, 0, 0
-    rows, _, half = rope.shape
-    if not rows or not half:                         # without an address it would mean no rotation
-        raise ValueError("a table of angles has rows and columns")
-    return _dense(rope, torch.float32, rows * 2 * half), rows, 2 * half
+def _weights(shape: PagedShape, w_q, w_k, eps):
+    dt, dim = shape.torch_dtype, shape.head_dim
+    return None if w_q is None else _dense(w_q, dt, dim), None if w_k is None else _dense(w_k, dt, dim), eps
 
 
 def halo_paged_append(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, rope=None,
                       rope_pairs: bool = False, seq=None, stream=None) -> None:
     """q [N][n_heads][head_dim] (or None, with q_out), k, v [N][n_kv_heads][head_dim]; rope as halo_rope_table gives it, on the
     device; seq None: token i belongs to sequence i."""
-    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
-    rc = load_library().halo_paged_append(shape.c, *new, *_angles(rope), 1 if rope_pairs else 0, po, _pool(k_pages, shape), _pool(v_pages, shape),
-                                          _stream(stream))
-    if rc:
-        raise HaloError("halo_paged_append", rc)
+    _append("halo_paged_append", shape, q, k, v, pos, page_table, k_pages, v_pages, q_out, rope, rope_pairs, seq, stream)
 
 
 def halo_paged_append_norm(shape: PagedShape, q, k, v, pos, page_table, k_pages, v_pages, q_out=None, w_q=None, w_k=None, eps: float = 1e-5,
                            rope=None, rope_pairs: bool = False, seq=None, stream=None) -> None:
     """halo_paged_append with the heads of queries and keys normed; w_q, w_k [head_dim] or None (1)."""
-    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
-    dt, dim = shape.torch_dtype, shape.head_dim
-    rc = load_library().halo_paged_append_norm(
-        shape.c, *new, None if w_q is None else _dense(w_q, dt, dim), None if w_k is None else _dense(w_k, dt, dim), eps, *_angles(rope),
-        1 if rope_pairs else 0, po, _pool(k_pages, shape), _pool(v_pages, shape), _stream(stream))
-    if rc:
-        raise HaloError("halo_paged_append_norm", rc)
+    _append("halo_paged_append_norm", shape, q, k, v, pos, page_table, k_pages, v_pages, q_out, rope, rope_pairs, seq, stream,
+            _weights(shape, w_q, w_k, eps))
 
 
 def halo_paged_append_q8(shape: PagedShape, q, k, v, pos, page_table, k_pool, v_pool, q_out=None, qk_norm: bool = False, w_q=None, w_k=None,
                          eps: float = 1e-5, rope=None, rope_pairs: bool = False, seq=None, stream=None) -> None:
     """The append into a cache of codes: k_pool, v_pool are pairs (codes int8 [n_pages][n_kv_heads][page_size][head_dim], scales float32
     [n_pages][n_kv_heads][page_size])."""
-    new, po = _new_tokens(shape, q, k, v, pos, page_table, q_out, seq)
-    dt, dim = shape.torch_dtype, shape.head_dim
-    rc = load_library().halo_paged_append_q8(
-        shape.c, *new, 1 if qk_norm else 0, None if w_q is None else _dense(w_q, dt, dim), None if w_k is None else _dense(w_k, dt, dim), eps,
-        *_angles(rope), 1 if rope_pairs else 0, po, *_pool_q8(k_pool, shape), *_pool_q8(v_pool, shape), _stream(stream))
-    if rc:
-        raise HaloError("halo_paged_append_q8", rc)
+    _append("halo_paged_append_q8", shape, q, k, v, pos, page_table, k_pool, v_pool, q_out, rope, rope_pairs, seq, stream,
+            (1 if qk_norm else 0, *_weights(shape, w_q, w_k, eps)), True)
 
 
 def halo_paged_read_q8(shape: PagedShape, pos, page_table, k_pool, v_pool, k_out, v_out, seq=None, stream=None) -> None:
