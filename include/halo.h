@@ -456,14 +456,15 @@ int halo_paged_append_norm(const halo_paged_shape *shape, int32_t N, const void 
  * queries and results.
  *
  * halo_paged_append_q8: halo_paged_append (qk_norm == 0; w_q, w_k and eps are then ignored) or halo_paged_append_norm (qk_norm != 0) into such a cache.  What becomes
- * a code is computed in double up to its rounding, from the inputs and the table of angles as they are.  Errors: as theirs; HALO_ERR_ARG also for scales misaligned to 4 bytes.
+ * a code is computed in double up to its rounding, from the inputs and the table of angles as they are.  Two tokens of one position of one page may leave codes of one and the scale of the other.  Errors: as theirs; HALO_ERR_ARG also for scales misaligned to 4 bytes.
  *
  * halo_paged_read_q8: what the rows of N tokens (pos, seq as in halo_paged_append) stand for, k_out, v_out [N][n_kv_heads][head_dim] dtype, computed in float; 0 for tokens that are padding.  Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N < 0, n_seq < 1, misaligned
  * pointers), HALO_ERR_HIP.
  *
  * halo_paged_attention_q8: halo_paged_attention over such a cache (with halo_paged_workspace_bytes).  Products are of the codes themselves, a key's scale multiplies its score, a
  * value's its probability; float queries and all probabilities enter the products as three bf16 values, which hold all of their bits (of
- * numbers from 2^-110 on: parts below 2^-126 count as 0).
+ * numbers from 2^-110 on: parts below 2^-126 count as 0).  Sums may overflow where a query's elements pass 2^113 (a code is up to 127, before its scale), and where values s c pass
+ * 2^120 / lens[t] (each term is up to 2^8 times its value until the division).
  */
 int halo_paged_append_q8(const halo_paged_shape *shape, int32_t N, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                          const void *v, int64_t v_stride, const int32_t *pos, const int32_t *seq, int32_t n_seq,
@@ -488,20 +489,20 @@ int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void
  * as halo_paged_attention, each token up to itself; a row's result does not depend on what later positions hold (NaN and infinities among it), nor on what other rows hold.  One to three launches.
  *   q [N][n_heads][head_dim]: dense heads, tokens q_stride elements apart; out [N][n_heads][head_dim] dense
  *   starts [n_seq + 1], non-decreasing, lens [n_seq], page_table [n_seq][max_pages] int32 on the device.  Rows before starts[0] and from starts[n_seq] on are
- *       left as they are; a sequence may have none.  Rows outside 0 .. N-1 do not exist.
+ *       left as they are; a sequence may have none.  Rows outside 0 .. N-1 do not exist and are not counted.
  *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
  *   mask [N][n_heads] uint8: a head whose byte is 0 gives out = 0; NULL = all survive.
  * Positions in pages that are no pages count as absent; a row without positions (also: more rows than positions) gives out = 0; scores that are all -infinity give NaN.
  * An infinite value gives its element of the rows that see it that infinity, or NaN where its probability is 0: a score of -infinity, or of a float below 2^-126 (against the largest score).
  * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16 (by 2^-8 of each at most; halo_paged_attention keeps all their bits); float queries, keys, values and probabilities
  * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (an infinite
- * float key or query gives NaN).  Sums of values hold up to 2^8 times their weights until they are divided: values of 2^120 and more may overflow.
+ * float key or query gives NaN).  Sums of values are divided last, and each of their terms is up to 2^8 times its value until then: values above 2^120 / (p + 1) may overflow.
  * Parts below 2^-126 count as 0: floats below 2^-110 enter with fewer bits.
  * _q8: over a cache of codes, as halo_paged_attention_q8.
- * How the work is cut depends on the arguments that the host sees and on the lengths; results do not depend on timing.
+ * How the work is cut, and with it a result's last bits, depends on the arguments that the host sees, on the lengths and, where scores are many, on the rows that the mask keeps; results do not depend on timing.
  * Errors: HALO_ERR_NULL, HALO_ERR_SHAPE, HALO_ERR_DTYPE, HALO_ERR_ARG (N outside 0..2^21, n_seq outside 0..4096, max_len, stride, alignment, scale not
- * finite), HALO_ERR_WORKSPACE, HALO_ERR_HIP.  halo_paged_chunk_workspace_bytes: the workspace of up to N tokens of up to n_seq sequences; 0 for invalid
- * arguments.
+ * finite), HALO_ERR_WORKSPACE, HALO_ERR_HIP.  halo_paged_chunk_workspace_bytes: the workspace of up to N tokens of up to n_seq sequences, with or without a mask: partial results of
+ * 512 KiB times head_dim, whatever N and n_seq, and 4 bytes for each token and head; 0 for invalid arguments.
  */
 size_t halo_paged_chunk_workspace_bytes(const halo_paged_shape *shape, int32_t N, int32_t n_seq);
 

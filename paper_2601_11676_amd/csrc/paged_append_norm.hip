@@ -2,9 +2,9 @@
 // eight bits with a scale for each row of a head (halo_paged_append_q8); what such rows stand for (halo_paged_read_q8).
 //     n(z) = z / sqrt(mean(z^2) + eps) * w,  then  (a, b) -> (a cos - b sin, b cos + a sin)
 //     s = max|x| / 127,  c = rint(x / s),  standing for s c
-// Each element moves once and its row's sum or maximum is exchanged between the lanes that hold it; few tokens are a launch and two round trips (3.7 us, of codes 5.1).  A row of
-// a head is 2^n neighbouring lanes of a wave, two pieces of 16 bytes each (a head of 80 leaves lanes idle).  Bytes bound the rows: 4099 tokens of 64 + 8 + 8 heads of 128, 170 MB, 34.3 us
-// with the call's gap, 4.9 TB/s (a copy of 4 GiB reaches 4.7).  The codes are bound by their instructions: 3001 tokens of 120 heads, 154 MB, 50 us, the VALU issuing 77 % of it.
+// Each element moves once and its row's sum or maximum is exchanged between the lanes that hold it; few tokens are a launch and two round trips (3.2 us, of codes 5.0).  A row of
+// a head is 2^n neighbouring lanes of a wave, two pieces of 16 bytes each (a head of 80 leaves lanes idle).  Bytes bound the rows: 4099 tokens of 64 + 8 + 8 heads of 128, 170 MB, 35 us
+// with the call's gap, 4.9 TB/s (a copy of 4 GiB reaches 4.7).  The codes are bound by their instructions: 3001 tokens of 120 heads, 154 MB, 51 us, the VALU issuing 78 % of it.
 //
 // A code is a decision: next to the border of two of them an error of the last bit moves the value by a whole step.  So what becomes a code is computed in double from
 // the inputs on; rows that come as they are, values among them, are exact as floats; what does not become a code is computed in float, rounded once.

@@ -1,8 +1,8 @@
 // Attention of chunks of new tokens over a paged cache (halo_paged_chunk_attention, halo_paged_chunk_attention_q8): token i of a sequence, at position p_i, has
 //     o_h = sum_j p_j V_j,  p = softmax_j(scale q_h . K_j),  j <= p_i
 // one pass over the rows with the running maximum and sum of the softmax.  Products bound it: a cached row meets all the rows of a block, 32, 128 or 256 queries (the heads of
-// one cache head, token by token).  512 tokens after 16000, 64 heads over 8 cache heads of 128, bf16: 278 us with the join, 980 TFLOP/s, where a library product of 8192^3 reaches 1230;
-// over codes 8192 tokens after as many 2.66 ms, 877 TFLOP/s.  In the attending kernel the matrix cores are busy 49 % of the time and the VALU issues 46 %: two waves of a SIMD,
+// one cache head, token by token).  512 tokens after 16000, 64 heads over 8 cache heads of 128, bf16: 279 us with the join, 978 TFLOP/s, where a library product of 8192^3 reaches 1230;
+// over codes 8192 tokens after as many 2.72 ms, 859 TFLOP/s (medians; from card to card 270 to 291 us, 2.64 to 2.77 ms).  In the attending kernel the matrix cores are busy 51 % of the time and the VALU issues 47 %: two waves of a SIMD,
 // each multiplying (1024 cycles a tile of 64 tokens) and taking exponentials (about as long) in turn.
 //
 // S^T = K Q^T      rows = tokens, columns = queries (matrix instruction of 32 x 32, 16 deep): a lane's results are scores of one query, so that maximum and sum

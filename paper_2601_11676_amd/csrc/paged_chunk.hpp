@@ -938,7 +938,8 @@ int launch_rows(ChunkArgs a, hipStream_t s)
     grid = (grid + kDies - 1) / kDies * kDies;
     // Blocks of the surviving rows alone save their share of the products, and cost a launch and blocks that end where their sequence does more often.  us, without / with the list:
     // 7 sequences of 4099 in all, 40 heads, three quarters of them kept (1.5e8 scores of the longest sequence) 77 / 85; 4 of 4000, 32 heads, half (2e8) 79 / 72; one of 4096 (5e8)
-    // 172 / 147, of 8192 564 / 353, with three quarters 561 / 482; 2 of 4000 after 2000, 64 heads, 8 cache heads, half 372 / 234.
+    // 172 / 147, of 8192 564 / 353, with three quarters 540 / 465; 2 of 4000 in all after 2000, 64 heads, 8 cache heads, half 372 / 234, three quarters 355 / 302.  With nearly all kept it costs: 31 of
+    // 32 heads, one of 4096 150 / 165, of 8192 550 / 569, 2 of 4000 after 2000 355 / 373.
     if (!a.mask || (int64_t)a.N * a.n_heads * a.max_len < 200000000) {
         a.kept = nullptr;
     } else {
