@@ -493,7 +493,7 @@ int halo_paged_attention_q8(const halo_paged_shape *shape, int32_t T, const void
  *   max_len: the longest of lens as far as the host knows it, 1 .. max_pages * page_size; longer ones count as max_len, negative ones as 0.
  *   mask [N][n_heads] uint8: a head whose byte is 0 gives out = 0; NULL = all survive.
  * Positions in pages that are no pages count as absent; a row without positions (also: more rows than positions) gives out = 0; scores that are all -infinity give NaN.
- * An infinite value gives its element of the rows that see it that infinity, or NaN where its probability is 0: a score of -infinity, or of a float below 2^-126 (against the largest score).
+ * An infinite value gives its element of the rows that see it that infinity; NaN where its score is -infinity; NaN or the infinity where its probability is below 2^-126 of the largest one's.
  * Scores, softmax and sums are float32.  A bf16 row's probabilities enter the product with the values rounded to bf16 (by 2^-8 of each at most; halo_paged_attention keeps all their bits); float queries, keys, values and probabilities
  * enter their products as three bf16 values each, of which products of less than 2^-24 of the whole are left out (an infinite
  * float key or query gives NaN).  Sums of values are divided last, and each of their terms is up to 2^8 times its value until then: values above 2^120 / (p + 1) may overflow.
